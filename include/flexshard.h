@@ -558,6 +558,134 @@ fs_status fs_seq_grad_bwd_update(
     void* stream, int32_t* dev_status);
 
 /*
+ * The rows of a sequence batch between the lookup and its gradient (Section 2,
+ * "Sequence embeddings": the unpooled rows feed a sequence model; Section 3.2
+ * metric 4, "dynamic memory": those activations are what a training step has
+ * to hold).  All three operators work on [n, D] rows as fs_seq_gather_fwd
+ * writes them and fs_seq_grad_bwd reads their gradient; D * sizeof(dtype) is a
+ * multiple of 16 and row pointers are 16-byte aligned as there.  Sums,
+ * statistics, states and the gradients of weights are float32; outputs in
+ * `dtype` are rounded once, to nearest even.  Outputs may not overlap inputs
+ * unless it says so.
+ *
+ * fs_seq_pack8 -- rows as 8-bit checkpoints.  Every block of 32 consecutive
+ *   columns of a row (the last block of a row may be shorter) gets one byte
+ *   exps[i * ceil(D / 32) + column / 32] = E and a signed byte codes[i * D + d]
+ *   a value: x ~ code * 2^(E - 133), ties to even.  E is in 1..254, the
+ *   smallest with which the block's largest magnitude rounds to at most 127
+ *   (E = 254: codes stop at +-127), so a code is off by at most half a step of
+ *   at most 1/64 of that magnitude.  E = 255: the block holds an infinity or a
+ *   NaN; it keeps those (codes +-127 and -128), its finite values become 0.
+ *   The result depends on the values of x alone: not on dtype, n or D.
+ * fs_seq_unpack8 -- x from codes and exps.  The values are exact in fp32 and
+ *   bf16; in fp16 one past its largest finite number is that number, and
+ *   subnormals are rounded.  Any bytes are taken (E = 0 as E = 1).
+ *   Host faults of both: unknown dtype; n < 0, n >= 2^31, D < 1 (FS_ERR_SIZE);
+ *   NULL; alignment as fs_seq_gather_fwd, codes 4-byte (fp32) or 8-byte aligned.
+ */
+fs_status fs_seq_pack8(
+    const void* x, int64_t n, int32_t D, fs_dtype dtype, int8_t* codes, uint8_t* exps, void* stream);
+
+fs_status fs_seq_unpack8(
+    const int8_t* codes, const uint8_t* exps, int64_t n, int32_t D, fs_dtype dtype, void* x, void* stream);
+
+/*
+ * fs_seq_norm_fwd -- layer norm of the rows:
+ *   mean[i] = sum_d x[i, d] / D,  rstd[i] = 1 / sqrt(sum_d (x[i, d] - mean[i])^2 / D + eps),
+ *   y[i, d] = (x[i, d] - mean[i]) * rstd[i] * gamma[d] + beta[d].
+ *   gamma[D], beta[D], mean[n], rstd[n] are float32.  mean and rstd (both or
+ *   neither) are what the backward pass needs; codes and exps (both or neither)
+ *   receive x as fs_seq_pack8 writes it, in the same pass.  y may be x.
+ * fs_seq_norm_bwd -- with u = (x - mean) rstd and g = dy gamma:
+ *   dx[i, d] = rstd[i] (g[i, d] - sum_d g / D - u[i, d] sum_d g u / D),
+ *   dgamma[d] = sum_i dy[i, d] u[i, d],  dbeta[d] = sum_i dy[i, d]   (overwritten)
+ *   dx may be dy.  The same bits on every run (no atomics).
+ * fs_seq_norm_bwd_packed -- the same with x given as a checkpoint (codes, exps
+ *   of fs_seq_pack8 or fs_seq_norm_fwd); mean and rstd are those of the rows
+ *   themselves.
+ *   Host faults: unknown dtype; n < 0, n >= 2^31, D < 1 (FS_ERR_SIZE); eps not
+ *   positive and finite (FS_ERR_CONFIG); NULL; alignment as above, gamma and
+ *   beta 16-byte aligned too; workspace as everywhere.  n == 0: the backward
+ *   pass writes zeros to dgamma and dbeta.
+ */
+fs_status fs_seq_norm_fwd(
+    const void* x, int64_t n, int32_t D, fs_dtype dtype, const float* gamma, const float* beta, float eps,
+    void* y, float* mean, float* rstd, int8_t* codes, uint8_t* exps, void* stream);
+
+fs_status fs_seq_norm_bwd(
+    const void* dy, const void* x, const float* mean, const float* rstd,
+    int64_t n, int32_t D, fs_dtype dtype, const float* gamma,
+    void* dx, float* dgamma, float* dbeta,
+    void* workspace, size_t* workspace_bytes /* host */, void* stream);
+
+fs_status fs_seq_norm_bwd_packed(
+    const void* dy, const int8_t* codes, const uint8_t* exps, const float* mean, const float* rstd,
+    int64_t n, int32_t D, fs_dtype dtype, const float* gamma,
+    void* dx, float* dgamma, float* dbeta,
+    void* workspace, size_t* workspace_bytes /* host */, void* stream);
+
+/*
+ * fs_seq_scan_fwd -- gated linear recurrence along every sequence of a jagged
+ * batch (offsets, T, B as in fs_route_bucketize: sequence s = t*B + b is rows
+ * offsets[s] .. offsets[s + 1] - 1, n = offsets[T*B]).  Per column, with
+ * f_t = 1 / (1 + exp(-gate[t, d])):
+ *   h_t = f_t h_(t-1) + (1 - f_t) x[t, d],  h before the first row = h0[s, d], or 0 if h0 is NULL.
+ *   h[n, D] in `dtype`; the recurrence itself runs on unrounded float32 states.
+ *   h0[T*B, D], h_last[T*B, D] float32; h_last (may be NULL) = the state after
+ *   the last row, of an empty sequence its h0 (or 0).  A gate of -infinity
+ *   shuts out the state before it, one of +infinity keeps it.  h may be x.
+ * fs_seq_scan_bwd -- gradients for dh[n, D] (of h) and dh_last (of h_last, may
+ *   be NULL = 0), backwards along every sequence:
+ *   G_t = dh_t + f_(t+1) G_(t+1)  (the last row: dh_t + dh_last[s]),
+ *   dx_t = (1 - f_t) G_t,  dgate_t = G_t (h_(t-1) - x_t) f_t (1 - f_t),
+ *   dh0[s] = f_first G_first (an empty sequence: dh_last[s] or 0; dh0 may be NULL).
+ *   x, gate, h as the forward pass had and wrote them (h_(t-1) is read in
+ *   `dtype`, h0 of the first row in float32).  dx or dgate may be dh.
+ * fs_seq_scan_bwd_packed -- the same with x, gate and h given as checkpoints of
+ *   fs_seq_pack8: 3 bytes a value and column held for the backward pass
+ *   instead of 6 or 12.
+ * fs_seq_scan_step -- one row for each of m sequences (serving a token at a
+ *   time): state_out = f state + (1 - f) x, h = state_out in `dtype`.
+ *   state[m, D], state_out[m, D] float32; state_out may be state, h may be x.
+ *
+ * Non-finite values of one sequence do not reach another.  Rows at or past n
+ * are neither read nor written.
+ * Data faults: bad offsets (FS_DEV_BAD_OFFSETS) leave the outputs unspecified
+ * but written in bounds.
+ * Host faults: unknown dtype; n < 0, n >= 2^31, D < 1, T < 1, B < 1,
+ * T*B >= 2^31 (FS_ERR_SIZE); NULL; alignment as above, h0, h_last, dh_last,
+ * dh0 and the states 16-byte aligned too; workspace as everywhere.
+ */
+fs_status fs_seq_scan_fwd(
+    const void* x, const void* gate, int64_t n, int32_t D, fs_dtype dtype,
+    const int64_t* offsets, int32_t T, int32_t B, const float* h0,
+    void* h, float* h_last,
+    void* workspace, size_t* workspace_bytes /* host */,
+    void* stream, int32_t* dev_status);
+
+fs_status fs_seq_scan_bwd(
+    const void* dh, const float* dh_last, const void* x, const void* gate, const void* h,
+    int64_t n, int32_t D, fs_dtype dtype,
+    const int64_t* offsets, int32_t T, int32_t B, const float* h0,
+    void* dx, void* dgate, float* dh0,
+    void* workspace, size_t* workspace_bytes /* host */,
+    void* stream, int32_t* dev_status);
+
+fs_status fs_seq_scan_bwd_packed(
+    const void* dh, const float* dh_last,
+    const int8_t* x_codes, const uint8_t* x_exps, const int8_t* gate_codes, const uint8_t* gate_exps,
+    const int8_t* h_codes, const uint8_t* h_exps,
+    int64_t n, int32_t D, fs_dtype dtype,
+    const int64_t* offsets, int32_t T, int32_t B, const float* h0,
+    void* dx, void* dgate, float* dh0,
+    void* workspace, size_t* workspace_bytes /* host */,
+    void* stream, int32_t* dev_status);
+
+fs_status fs_seq_scan_step(
+    const void* x, const void* gate, int64_t m, int32_t D, fs_dtype dtype, const float* state,
+    float* state_out, void* h, void* stream);
+
+/*
  * fs_cost_model -- the analytical per-GPU costs of one sequence embedding
  * table in one training iteration under a uniform strategy (Section 3.2: the
  * six metrics; the memory-cost and communication-cost tables, cell by cell).

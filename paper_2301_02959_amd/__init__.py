@@ -35,6 +35,8 @@ EXPORTS = ["fs_route_bucketize", "fs_route_bucketize_noalloc", "fs_seq_gather_fw
            "fs_sort_lookups", "fs_seq_grad_bwd_sorted", "fs_seq_gather_fwd_sorted", "fs_seq_grad_bwd_update",
            "fs_seq_gather_send", "fs_seq_unbucketize", "fs_replica_build", "fs_seq_gather_fwd_replica", "fs_plan_tiers",
            "fs_replica_tag_slots", "fs_route_bucketize_slots", "fs_seq_gather_fwd_slots",
+           "fs_seq_pack8", "fs_seq_unpack8", "fs_seq_norm_fwd", "fs_seq_norm_bwd", "fs_seq_norm_bwd_packed",
+           "fs_seq_scan_fwd", "fs_seq_scan_bwd", "fs_seq_scan_bwd_packed", "fs_seq_scan_step",
            "fs_cost_model", "fs_tier_traffic", "fs_sparse_update", "fs_util_copy", "fs_util_read_write_mix", "fs_version", "fs_bwd_tile", "fs_prof_begin", "fs_prof_only", "fs_prof_end"]
 
 _DTYPES = {torch.float32: FS_F32, torch.float16: FS_F16, torch.bfloat16: FS_BF16}
@@ -72,6 +74,7 @@ def lib() -> ctypes.CDLL:
 
 _P, _I, _L, _F, _Z = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.POINTER(ctypes.c_size_t)
 _ROUTE = [_P, _P, _I, _I, _P, _P, _L, _I, _I, _I, _P, _P, _P]
+_SCAN = [_L, _I, _I, _P, _I, _I]
 _SIGNATURES = {
     "fs_route_bucketize": _ROUTE + [_P, _P, _Z, _P, _P],
     "fs_route_bucketize_noalloc": _ROUTE + [_P, _P, _P],
@@ -91,6 +94,15 @@ _SIGNATURES = {
     "fs_plan_tiers": [_P, _L, _P, _I, _P, _L, _P, _P, _P, _Z, _P, _P],
     "fs_sparse_update": [_P, _L, _I, _I, _P, _P, _L, _P, _I, _F, _F, _P, _P, _P, _L, _P, _P],
     "fs_seq_grad_bwd_update": [_P, _L, _I, _I, _P, _P, _L, _L, _P, _I, _F, _F, _P, _P, _P, _L, _P, _P, _L, _P, _P, _Z, _P, _P],
+    "fs_seq_pack8": [_P, _L, _I, _I, _P, _P, _P],
+    "fs_seq_unpack8": [_P, _P, _L, _I, _I, _P, _P],
+    "fs_seq_norm_fwd": [_P, _L, _I, _I, _P, _P, _F] + [_P] * 6,
+    "fs_seq_norm_bwd": [_P, _P, _P, _P, _L, _I, _I, _P, _P, _P, _P, _P, _Z, _P],
+    "fs_seq_norm_bwd_packed": [_P, _P, _P, _P, _P, _L, _I, _I, _P, _P, _P, _P, _P, _Z, _P],
+    "fs_seq_scan_fwd": [_P, _P] + _SCAN + [_P, _P, _P, _P, _Z, _P, _P],
+    "fs_seq_scan_bwd": [_P] * 5 + _SCAN + [_P, _P, _P, _P, _P, _Z, _P, _P],
+    "fs_seq_scan_bwd_packed": [_P] * 8 + _SCAN + [_P, _P, _P, _P, _P, _Z, _P, _P],
+    "fs_seq_scan_step": [_P, _P, _L, _I, _I, _P, _P, _P, _P],
     "fs_util_copy": [_P, _P, _L, _P],
     "fs_util_read_write_mix": [_P, _L, _I, _P, _L, _P],
 }
@@ -117,6 +129,8 @@ _I32 = (torch.int32,)
 _U32 = (torch.int32, torch.uint32)          # 32-bit words: torch code usually holds them as int32
 _F32 = (torch.float32,)
 _ROWS = (torch.float32, torch.float16, torch.bfloat16)
+_I8 = (torch.int8,)
+_U8 = (torch.uint8,)
 
 
 def _ptr_checked(t: Optional[torch.Tensor], dtypes: Optional[tuple] = None) -> Optional[int]:
@@ -498,6 +512,172 @@ def fs_seq_grad_bwd_update(grad_out, sorted_rows, sorted_pos, m: int, R: int, we
     else:
         size = ctypes.c_size_t(workspace.numel())
     return _check("fs_seq_grad_bwd_update", call(_ptr(workspace), ctypes.byref(size)), raise_on_error)
+
+
+def _like(fn: str, rows: torch.Tensor, same=(), float_rows=(), columns=(), per_row=(), packed=()) -> Tuple[int, int, int]:
+    """(n, D, dtype) of `rows`, once the tensors that go with it are found to be of its sizes, its type and its device, which
+    has to be the current one (the stream is).  The library takes sizes from the caller, so a tensor that is too small would
+    be read past its end.  same: [n, D] in the type of rows; float_rows: [n, D] float32; columns: [D] float32;
+    per_row: [n] float32; packed: pairs of codes [n, D] and exps [n, ceil(D / 32)]."""
+    if rows.dim() != 2:
+        raise ValueError(f"{fn}: rows are [n, D], got {tuple(rows.shape)}")
+    n, D = rows.shape
+    if rows.dtype not in _DTYPES:
+        raise TypeError(f"{fn}: rows are float32, float16 or bfloat16, got {rows.dtype}")
+    where = rows.get_device()
+    if where >= 0 and where != _raw_device():
+        raise ValueError(f"{fn}: tensors on device {where}, the current device is {_raw_device()}")
+
+    def need(t, shape, dtype):
+        if t is not None and (tuple(t.shape) != shape or t.dtype != dtype or t.get_device() != where):
+            raise ValueError(f"{fn}: expected {dtype} of shape {shape} on the device of the rows, got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+    for t in same:
+        need(t, (n, D), rows.dtype)
+    for t in float_rows:
+        need(t, (n, D), torch.float32)
+    for t in columns:
+        need(t, (D,), torch.float32)
+    for t in per_row:
+        need(t, (n,), torch.float32)
+    for codes, exps in packed:
+        need(codes, (n, D), torch.int8)
+        need(exps, (n, (D + 31) // 32), torch.uint8)
+    return n, D, _DTYPES[rows.dtype]
+
+
+def fs_seq_pack8(x, codes, exps, raise_on_error: bool = True) -> int:
+    n, D, dtype = _like("fs_seq_pack8", x, packed=((codes, exps),))
+    code = _typed().fs_seq_pack8(_ptr(x, _ROWS), n, D, dtype, _ptr(codes, _I8), _ptr(exps, _U8), _stream())
+    return _check("fs_seq_pack8", code, raise_on_error)
+
+
+def fs_seq_unpack8(codes, exps, x, raise_on_error: bool = True) -> int:
+    n, D, dtype = _like("fs_seq_unpack8", x, packed=((codes, exps),))
+    code = _typed().fs_seq_unpack8(_ptr(codes, _I8), _ptr(exps, _U8), n, D, dtype, _ptr(x, _ROWS), _stream())
+    return _check("fs_seq_unpack8", code, raise_on_error)
+
+
+def fs_seq_norm_fwd(x, gamma, beta, eps: float, y, mean=None, rstd=None, codes=None, exps=None,
+                    raise_on_error: bool = True) -> int:
+    n, D, dtype = _like("fs_seq_norm_fwd", x, same=(y,), columns=(gamma, beta), per_row=(mean, rstd), packed=((codes, exps),))
+    code = _typed().fs_seq_norm_fwd(
+        _ptr(x, _ROWS), n, D, dtype, _ptr(gamma, _F32), _ptr(beta, _F32), eps, _ptr(y, _ROWS), _ptr(mean, _F32),
+        _ptr(rstd, _F32), _ptr(codes, _I8), _ptr(exps, _U8), _stream())
+    return _check("fs_seq_norm_fwd", code, raise_on_error)
+
+
+def _with_workspace(fn: str, call, device, workspace: Optional[torch.Tensor], raise_on_error: bool) -> int:
+    """call(workspace pointer, its size) with the caller's workspace, or one of the size that the entry point asks for."""
+    if workspace is None:
+        workspace, size, code = _workspace(call, device)
+        if code != 0:
+            return _check(fn, code, raise_on_error)
+    else:
+        size = ctypes.c_size_t(workspace.numel() * workspace.element_size())
+    return _check(fn, call(_ptr(workspace), ctypes.byref(size)), raise_on_error)
+
+
+def fs_seq_norm_bwd(dy, x, mean, rstd, gamma, dx, dgamma, dbeta, workspace: Optional[torch.Tensor] = None,
+                    raise_on_error: bool = True) -> int:
+    n, D, dtype = _like("fs_seq_norm_bwd", dy, same=(x, dx), columns=(gamma, dgamma, dbeta), per_row=(mean, rstd))
+    L = _typed()
+    args = (_ptr(dy, _ROWS), _ptr(x, _ROWS), _ptr(mean, _F32), _ptr(rstd, _F32), n, D, dtype, _ptr(gamma, _F32),
+            _ptr(dx, _ROWS), _ptr(dgamma, _F32), _ptr(dbeta, _F32))
+    stream = _stream()
+    return _with_workspace("fs_seq_norm_bwd", lambda ws, size: L.fs_seq_norm_bwd(*args, ws, size, stream), dy.device, workspace,
+                           raise_on_error)
+
+
+def fs_seq_norm_bwd_packed(dy, codes, exps, mean, rstd, gamma, dx, dgamma, dbeta, workspace: Optional[torch.Tensor] = None,
+                           raise_on_error: bool = True) -> int:
+    n, D, dtype = _like("fs_seq_norm_bwd_packed", dy, same=(dx,), columns=(gamma, dgamma, dbeta), per_row=(mean, rstd),
+                        packed=((codes, exps),))
+    L = _typed()
+    args = (_ptr(dy, _ROWS), _ptr(codes, _I8), _ptr(exps, _U8), _ptr(mean, _F32), _ptr(rstd, _F32), n, D, dtype,
+            _ptr(gamma, _F32), _ptr(dx, _ROWS), _ptr(dgamma, _F32), _ptr(dbeta, _F32))
+    stream = _stream()
+    return _with_workspace("fs_seq_norm_bwd_packed", lambda ws, size: L.fs_seq_norm_bwd_packed(*args, ws, size, stream), dy.device,
+                           workspace, raise_on_error)
+
+
+def seq_norm_bwd_workspace_bytes(n: int, D: int, dtype: int) -> int:
+    size = ctypes.c_size_t(0)
+    code = _typed().fs_seq_norm_bwd(None, None, None, None, n, D, dtype, None, None, None, None, None, ctypes.byref(size), None)
+    _check("fs_seq_norm_bwd", code, True)
+    return int(size.value)
+
+
+def _sequences(fn: str, rows, offsets, T: int, B: int, states) -> None:
+    """offsets[T*B + 1] and the [T*B, D] float32 states at the sequences' ends, on the device of the rows."""
+    where = rows.get_device()
+    if offsets.dim() != 1 or offsets.shape[0] != T * B + 1 or offsets.get_device() != where:
+        raise ValueError(f"{fn}: expected {T * B + 1} offsets on the device of the rows, got {tuple(offsets.shape)} on {offsets.device}")
+    for t in states:
+        if t is not None and (tuple(t.shape) != (T * B, rows.shape[1]) or t.get_device() != where):
+            raise ValueError(f"{fn}: states are [{T * B}, {rows.shape[1]}] on the device of the rows, got {tuple(t.shape)} on {t.device}")
+
+
+def fs_seq_scan_fwd(x, gate, offsets, T: int, B: int, h0, h, h_last=None, dev_status=None,
+                    workspace: Optional[torch.Tensor] = None, raise_on_error: bool = True) -> int:
+    n, D, dtype = _like("fs_seq_scan_fwd", x, same=(gate, h))
+    _sequences("fs_seq_scan_fwd", x, offsets, T, B, (h0, h_last))
+    L = _typed()
+    args = (_ptr(x, _ROWS), _ptr(gate, _ROWS), n, D, dtype, _ptr(offsets, _I64), T, B, _ptr(h0, _F32), _ptr(h, _ROWS),
+            _ptr(h_last, _F32))
+    tail = (_stream(), _ptr(dev_status, _I32))
+    return _with_workspace("fs_seq_scan_fwd", lambda ws, size: L.fs_seq_scan_fwd(*args, ws, size, *tail), x.device, workspace,
+                           raise_on_error)
+
+
+def fs_seq_scan_bwd(dh, dh_last, x, gate, h, offsets, T: int, B: int, h0, dx, dgate, dh0=None, dev_status=None,
+                    workspace: Optional[torch.Tensor] = None, raise_on_error: bool = True) -> int:
+    n, D, dtype = _like("fs_seq_scan_bwd", dh, same=(x, gate, h, dx, dgate))
+    _sequences("fs_seq_scan_bwd", dh, offsets, T, B, (dh_last, h0, dh0))
+    L = _typed()
+    args = (_ptr(dh, _ROWS), _ptr(dh_last, _F32), _ptr(x, _ROWS), _ptr(gate, _ROWS), _ptr(h, _ROWS), n, D, dtype,
+            _ptr(offsets, _I64), T, B, _ptr(h0, _F32), _ptr(dx, _ROWS), _ptr(dgate, _ROWS), _ptr(dh0, _F32))
+    tail = (_stream(), _ptr(dev_status, _I32))
+    return _with_workspace("fs_seq_scan_bwd", lambda ws, size: L.fs_seq_scan_bwd(*args, ws, size, *tail), dh.device, workspace,
+                           raise_on_error)
+
+
+def fs_seq_scan_bwd_packed(dh, dh_last, x_codes, x_exps, gate_codes, gate_exps, h_codes, h_exps, offsets, T: int, B: int,
+                           h0, dx, dgate, dh0=None, dev_status=None, workspace: Optional[torch.Tensor] = None,
+                           raise_on_error: bool = True) -> int:
+    n, D, dtype = _like("fs_seq_scan_bwd_packed", dh, same=(dx, dgate),
+                        packed=((x_codes, x_exps), (gate_codes, gate_exps), (h_codes, h_exps)))
+    _sequences("fs_seq_scan_bwd_packed", dh, offsets, T, B, (dh_last, h0, dh0))
+    L = _typed()
+    args = (_ptr(dh, _ROWS), _ptr(dh_last, _F32), _ptr(x_codes, _I8), _ptr(x_exps, _U8), _ptr(gate_codes, _I8),
+            _ptr(gate_exps, _U8), _ptr(h_codes, _I8), _ptr(h_exps, _U8), n, D, dtype, _ptr(offsets, _I64), T, B,
+            _ptr(h0, _F32), _ptr(dx, _ROWS), _ptr(dgate, _ROWS), _ptr(dh0, _F32))
+    tail = (_stream(), _ptr(dev_status, _I32))
+    return _with_workspace("fs_seq_scan_bwd_packed", lambda ws, size: L.fs_seq_scan_bwd_packed(*args, ws, size, *tail), dh.device,
+                           workspace, raise_on_error)
+
+
+def seq_scan_fwd_workspace_bytes(n: int, D: int, dtype: int, T: int, B: int) -> int:
+    size = ctypes.c_size_t(0)
+    code = _typed().fs_seq_scan_fwd(None, None, n, D, dtype, None, T, B, None, None, None, None, ctypes.byref(size), None, None)
+    _check("fs_seq_scan_fwd", code, True)
+    return int(size.value)
+
+
+def seq_scan_bwd_workspace_bytes(n: int, D: int, dtype: int, T: int, B: int) -> int:
+    """The packed form needs the same."""
+    size = ctypes.c_size_t(0)
+    code = _typed().fs_seq_scan_bwd(None, None, None, None, None, n, D, dtype, None, T, B, None, None, None, None, None,
+                                    ctypes.byref(size), None, None)
+    _check("fs_seq_scan_bwd", code, True)
+    return int(size.value)
+
+
+def fs_seq_scan_step(x, gate, state, state_out, h, raise_on_error: bool = True) -> int:
+    n, D, dtype = _like("fs_seq_scan_step", x, same=(gate, h), float_rows=(state, state_out))
+    code = _typed().fs_seq_scan_step(_ptr(x, _ROWS), _ptr(gate, _ROWS), n, D, dtype, _ptr(state, _F32), _ptr(state_out, _F32),
+                                     _ptr(h, _ROWS), _stream())
+    return _check("fs_seq_scan_step", code, raise_on_error)
 
 
 class CostParams(ctypes.Structure):

@@ -1,0 +1,574 @@
+// fs_seq_norm_fwd, fs_seq_norm_bwd, fs_seq_norm_bwd_packed: layer norm of the rows of a sequence and its gradients.
+//
+//   forward   m = mean(x), v = mean((x - m)^2), r = 1 / sqrt(v + eps), y = (x - m) r gamma + beta
+//   backward  u = (x - m) r, g = dy gamma:  dx = r (g - mean(g) - u mean(g u)), dgamma = sum over rows of dy u, dbeta = of dy
+//
+// HBM-bound: x read once and y written once; dy and x (or its checkpoint) read once and dx written once.  A row of up to 256
+// pieces of 16 bytes lies in the registers of a group of G lanes, P pieces a lane, so mean and squares are two passes over
+// registers; longer rows are read three times by a workgroup each (kernels *_wide).  All sums are fp32.  The variance is taken
+// about the rounded mean and corrected by what that mean is off (s1 below), so a row of equal values far from zero
+// normalises to zeros.
+// dgamma and dbeta: every lane keeps its columns' sums over the rows that its group walks, a workgroup adds its groups in
+// LDS and writes one partial row, norm_grad_sum adds the partial rows in their order: no atomics, the same bits every run.
+#include "pack8.h"
+#include "seq_rows.h"
+
+namespace fs {
+
+struct NormArgs {
+    const u32x4* x;
+    const uint32_t* x_codes;         // packed backward: x as a checkpoint
+    const uint8_t* x_exps;
+    const u32x4* dy;
+    int64_t n;
+    int units;                       // 16-byte pieces of a row
+    int nb;                          // blocks of columns of a checkpoint's row
+    float inv_D;
+    float eps;
+    const float* gamma;
+    const float* beta;
+    u32x4* y;
+    float* mean;                     // forward: may be null
+    float* rstd;
+    uint32_t* codes;                 // forward: may be null
+    uint8_t* exps;
+    u32x4* dx;
+    float* partial;                  // [workgroups][2][D]
+};
+
+template <int N>
+__device__ __forceinline__ void load_floats(const float* p, float* v)
+{
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        const f32x4 q = *reinterpret_cast<const f32x4*>(p + i);
+        v[i] = q[0]; v[i + 1] = q[1]; v[i + 2] = q[2]; v[i + 3] = q[3];
+    }
+}
+
+// Writes a piece's codes; all lanes of the block of columns call it (in = false: a lane past the row's end).
+template <int DT, int G>
+__device__ __forceinline__ void write_codes(const NormArgs& a, int64_t row, int piece, bool in, const float* v)
+{
+    constexpr int N = Piece<DT>::N, LPB = kPackBlock / N, L = LPB < G ? LPB : G;
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t b = in ? __float_as_uint(v[i]) & 0x7FFFFFFFu : 0u;
+        top = top > b ? top : b;
+    }
+    const int E = pack_exponent(group_top<L>(top));
+    if (!in) return;
+    uint32_t* to = a.codes + (row * a.units + piece) * (N / 4);
+    if constexpr (N == 8) {
+        const u32x2 c = {pack_four(v, E), pack_four(v + 4, E)};
+        __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(to));
+    } else {
+        __builtin_nontemporal_store(pack_four(v, E), to);
+    }
+    if (piece % LPB == 0) a.exps[row * a.nb + piece / LPB] = (uint8_t)E;
+}
+
+// A group of G lanes takes U rows, all their loads in flight at once.
+template <int DT, int G, int P, int U, bool PACK>
+__global__ __launch_bounds__(kBlock) void norm_fwd_kernel(NormArgs a)
+{
+    constexpr int N = Piece<DT>::N, kGroups = kBlock / G;
+    const int lig = threadIdx.x % G, group = threadIdx.x / G;
+    const int64_t row0 = (int64_t)blockIdx.x * (kGroups * U) + group;
+    u32x4 raw[U][P];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int64_t row = row0 + u * kGroups;
+            const int piece = lig + p * G;
+            raw[u][p] = u32x4{0u, 0u, 0u, 0u};
+            if (row < a.n && piece < a.units) raw[u][p] = load_stream(a.x + row * a.units + piece);
+        }
+    float gamma[P][N], beta[P][N];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        const int piece = lig + p * G < a.units ? lig + p * G : 0;
+        load_floats<N>(a.gamma + (int64_t)piece * N, gamma[p]);
+        load_floats<N>(a.beta + (int64_t)piece * N, beta[p]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t row = row0 + u * kGroups;
+        float c[P][N];
+        float s = 0.0f;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            Piece<DT>::unpack(raw[u][p], c[p]);
+#pragma unroll
+            for (int i = 0; i < N; ++i) s += c[p][i];
+            if constexpr (PACK) write_codes<DT, G>(a, row, lig + p * G, row < a.n && lig + p * G < a.units, c[p]);
+        }
+        float mean = group_sum<G>(s) * a.inv_D;
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const bool in = lig + p * G < a.units;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                c[p][i] = in ? c[p][i] - mean : 0.0f;
+                s1 += c[p][i];
+                s2 = fmaf(c[p][i], c[p][i], s2);
+            }
+        }
+        const float off = group_sum<G>(s1) * a.inv_D;
+        const float var = fmaf(-off, off, group_sum<G>(s2) * a.inv_D);
+        const float rstd = 1.0f / sqrtf(fmaxf(var, 0.0f) + a.eps);
+        mean += off;
+        if (row >= a.n) continue;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            if (lig + p * G >= a.units) continue;
+            float y[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) y[i] = fmaf((c[p][i] - off) * rstd, gamma[p][i], beta[p][i]);
+            store_stream(a.y + row * a.units + lig + p * G, Piece<DT>::pack(y));
+        }
+        if (lig == 0 && a.mean != nullptr) { a.mean[row] = mean; a.rstd[row] = rstd; }
+    }
+}
+
+// Sum over the workgroup, the same bits in every thread; `lds` holds kWavesPerBlock floats.
+__device__ __forceinline__ float block_sum(float v, float* lds)
+{
+    v = group_sum<kWave>(v);
+    __syncthreads();                       // lds may still be read from a previous call
+    if (lane_id() == 0) lds[wave_id()] = v;
+    __syncthreads();
+    float s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWavesPerBlock; ++w) s += lds[w];
+    return s;
+}
+
+// Rows of more than 256 pieces, one workgroup a row; the second and third pass read what the first has brought into the L2.
+template <int DT, bool PACK>
+__global__ __launch_bounds__(kBlock) void norm_fwd_wide_kernel(NormArgs a)
+{
+    constexpr int N = Piece<DT>::N;
+    __shared__ float lds[kWavesPerBlock];
+    const int64_t row = blockIdx.x;
+    const u32x4* x = a.x + row * a.units;
+    float s = 0.0f;
+    for (int p0 = 0; p0 < a.units; p0 += kBlock) {
+        const int piece = p0 + (int)threadIdx.x;
+        float c[N];
+        u32x4 raw = {0u, 0u, 0u, 0u};
+        if (piece < a.units) raw = x[piece];
+        Piece<DT>::unpack(raw, c);
+#pragma unroll
+        for (int i = 0; i < N; ++i) s += c[i];
+        if constexpr (PACK) write_codes<DT, kWave>(a, row, piece, piece < a.units, c);
+    }
+    float mean = block_sum(s, lds) * a.inv_D;
+    float s1 = 0.0f, s2 = 0.0f;
+    for (int piece = threadIdx.x; piece < a.units; piece += kBlock) {
+        float c[N];
+        Piece<DT>::unpack(x[piece], c);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float d = c[i] - mean;
+            s1 += d;
+            s2 = fmaf(d, d, s2);
+        }
+    }
+    const float off = block_sum(s1, lds) * a.inv_D;
+    const float var = fmaf(-off, off, block_sum(s2, lds) * a.inv_D);
+    const float rstd = 1.0f / sqrtf(fmaxf(var, 0.0f) + a.eps);
+    for (int piece = threadIdx.x; piece < a.units; piece += kBlock) {
+        float c[N], gamma[N], beta[N];
+        Piece<DT>::unpack(x[piece], c);
+        load_floats<N>(a.gamma + (int64_t)piece * N, gamma);
+        load_floats<N>(a.beta + (int64_t)piece * N, beta);
+#pragma unroll
+        for (int i = 0; i < N; ++i) c[i] = fmaf((c[i] - mean - off) * rstd, gamma[i], beta[i]);
+        store_stream(a.y + row * a.units + piece, Piece<DT>::pack(c));
+    }
+    if (threadIdx.x == 0 && a.mean != nullptr) { a.mean[row] = mean + off; a.rstd[row] = rstd; }
+}
+
+// A piece of x for the backward pass, from the rows or from their checkpoint.
+template <int DT, bool PACKED>
+struct XPiece {
+    u32x4 raw;                       // PACKED: the codes in [0], [1]; the exponent in [2]
+    __device__ __forceinline__ void load(const NormArgs& a, int64_t row, int piece)
+    {
+        constexpr int N = Piece<DT>::N, LPB = kPackBlock / N;
+        if constexpr (PACKED) {
+            const uint32_t* from = a.x_codes + (row * a.units + piece) * (N / 4);
+            if constexpr (N == 8) {
+                const u32x2 c = load_stream(reinterpret_cast<const u32x2*>(from));
+                raw[0] = c[0]; raw[1] = c[1];
+            } else {
+                raw[0] = load_stream(from);
+            }
+            raw[2] = a.x_exps[row * a.nb + piece / LPB];
+        } else {
+            raw = load_stream(a.x + row * a.units + piece);
+        }
+    }
+    __device__ __forceinline__ void zero() { raw = u32x4{0u, 0u, 0u, 0u}; }
+    __device__ __forceinline__ void values(float* v) const
+    {
+        if constexpr (PACKED) {
+            const float step = __uint_as_float(pack_step_bits((int)raw[2]));
+            unpack_four(raw[0], (int)raw[2], step, v);
+            if constexpr (Piece<DT>::N == 8) unpack_four(raw[1], (int)raw[2], step, v + 4);
+        } else {
+            Piece<DT>::unpack(raw, v);
+        }
+    }
+};
+
+template <int DT, int G, int P, int U, bool PACKED>
+__global__ __launch_bounds__(kBlock) void norm_bwd_kernel(NormArgs a)
+{
+    constexpr int N = Piece<DT>::N, kGroups = kBlock / G;
+    __shared__ float lds[kGroups][2][G * N];
+    const int lig = threadIdx.x % G, group = threadIdx.x / G;
+    float gamma[P][N], dg[P][N], db[P][N];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        const int piece = lig + p * G < a.units ? lig + p * G : 0;
+        load_floats<N>(a.gamma + (int64_t)piece * N, gamma[p]);
+#pragma unroll
+        for (int i = 0; i < N; ++i) dg[p][i] = db[p][i] = 0.0f;
+    }
+    for (int64_t r0 = (int64_t)blockIdx.x * (kGroups * U); r0 < a.n; r0 += (int64_t)gridDim.x * (kGroups * U)) {
+        u32x4 dy_raw[U][P];
+        XPiece<DT, PACKED> x_raw[U][P];
+        float mean[U], rstd[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t row = r0 + u * kGroups + group;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const int piece = lig + p * G;
+                dy_raw[u][p] = u32x4{0u, 0u, 0u, 0u};
+                x_raw[u][p].zero();
+                if (row < a.n && piece < a.units) {
+                    dy_raw[u][p] = load_stream(a.dy + row * a.units + piece);
+                    x_raw[u][p].load(a, row, piece);
+                }
+            }
+            mean[u] = rstd[u] = 0.0f;
+            if (row < a.n) { mean[u] = a.mean[row]; rstd[u] = a.rstd[row]; }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t row = r0 + u * kGroups + group;
+            float w[P][N], g[P][N];                      // u of the formula, and dy gamma
+            float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const bool in = row < a.n && lig + p * G < a.units;
+                float dy[N];
+                x_raw[u][p].values(w[p]);
+                Piece<DT>::unpack(dy_raw[u][p], dy);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    w[p][i] = in ? (w[p][i] - mean[u]) * rstd[u] : 0.0f;
+                    dg[p][i] = fmaf(dy[i], w[p][i], dg[p][i]);
+                    db[p][i] += dy[i];
+                    g[p][i] = dy[i] * gamma[p][i];
+                    s1 += g[p][i];
+                    s2 = fmaf(g[p][i], w[p][i], s2);
+                }
+            }
+            const float m1 = group_sum<G>(s1) * a.inv_D, m2 = group_sum<G>(s2) * a.inv_D;
+            if (row >= a.n) continue;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                if (lig + p * G >= a.units) continue;
+                float dx[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) dx[i] = rstd[u] * fmaf(-w[p][i], m2, g[p][i] - m1);
+                store_stream(a.dx + row * a.units + lig + p * G, Piece<DT>::pack(dx));
+            }
+        }
+    }
+    const int64_t D = (int64_t)a.units * N;
+    float* to = a.partial + (int64_t)blockIdx.x * 2 * D;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        if (p > 0) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            lds[group][0][lig * N + i] = dg[p][i];
+            lds[group][1][lig * N + i] = db[p][i];
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < 2 * G * N; c += kBlock) {
+            const int which = c / (G * N), col = c % (G * N);
+            float s = 0.0f;
+#pragma unroll 4
+            for (int k = 0; k < kGroups; ++k) s += lds[k][which][col];
+            if (p * G * N + col < D) to[which * D + p * G * N + col] = s;
+        }
+    }
+}
+
+// dgamma and dbeta as the sums of the `rows` partial rows of 2 D columns: wave w of a workgroup adds rows w, w + 16, ... for
+// its 64 columns, then the 16 sums are added in order.
+constexpr int kGradSumWaves = 16;
+__global__ __launch_bounds__(kGradSumWaves * kWave) void norm_grad_sum_kernel(const float* __restrict__ partial, int64_t rows,
+                                                                             int64_t D, float* __restrict__ dgamma,
+                                                                             float* __restrict__ dbeta)
+{
+    __shared__ float lds[kGradSumWaves][kWave];
+    const int64_t col = (int64_t)blockIdx.x * kWave + lane_id();
+    float s = 0.0f;
+    if (col < 2 * D) {
+#pragma unroll 8
+        for (int64_t r = wave_id(); r < rows; r += kGradSumWaves) s += partial[r * 2 * D + col];
+    }
+    lds[wave_id()][lane_id()] = s;
+    __syncthreads();
+    if (wave_id() != 0 || col >= 2 * D) return;
+    s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kGradSumWaves; ++w) s += lds[w][lane_id()];
+    if (col < D) dgamma[col] = s; else dbeta[col - D] = s;
+}
+
+// Rows of more than 256 pieces: dx by a workgroup a row.
+template <int DT, bool PACKED>
+__global__ __launch_bounds__(kBlock) void norm_bwd_wide_kernel(NormArgs a)
+{
+    constexpr int N = Piece<DT>::N;
+    __shared__ float lds[kWavesPerBlock];
+    const int64_t row = blockIdx.x;
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float s1 = 0.0f, s2 = 0.0f;
+    for (int piece = threadIdx.x; piece < a.units; piece += kBlock) {
+        XPiece<DT, PACKED> xp;
+        xp.load(a, row, piece);
+        float x[N], dy[N], gamma[N];
+        xp.values(x);
+        Piece<DT>::unpack(a.dy[row * a.units + piece], dy);
+        load_floats<N>(a.gamma + (int64_t)piece * N, gamma);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float g = dy[i] * gamma[i];
+            s1 += g;
+            s2 = fmaf(g, (x[i] - mean) * rstd, s2);
+        }
+    }
+    const float m1 = block_sum(s1, lds) * a.inv_D, m2 = block_sum(s2, lds) * a.inv_D;
+    for (int piece = threadIdx.x; piece < a.units; piece += kBlock) {
+        XPiece<DT, PACKED> xp;
+        xp.load(a, row, piece);
+        float x[N], dy[N], gamma[N];
+        xp.values(x);
+        Piece<DT>::unpack(a.dy[row * a.units + piece], dy);
+        load_floats<N>(a.gamma + (int64_t)piece * N, gamma);
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = rstd * fmaf(-((x[i] - mean) * rstd), m2, dy[i] * gamma[i] - m1);
+        store_stream(a.dx + row * a.units + piece, Piece<DT>::pack(x));
+    }
+}
+
+// ... and the columns' sums over the rows r, r + gridDim.y, ... by workgroups of 256 pieces of columns.
+template <int DT, bool PACKED>
+__global__ __launch_bounds__(kBlock) void norm_cols_wide_kernel(NormArgs a)
+{
+    constexpr int N = Piece<DT>::N;
+    const int piece = (int)blockIdx.x * kBlock + (int)threadIdx.x;
+    if (piece >= a.units) return;
+    float dg[N], db[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) dg[i] = db[i] = 0.0f;
+    for (int64_t row = blockIdx.y; row < a.n; row += gridDim.y) {
+        XPiece<DT, PACKED> xp;
+        xp.load(a, row, piece);
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float x[N], dy[N];
+        xp.values(x);
+        Piece<DT>::unpack(a.dy[row * a.units + piece], dy);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            dg[i] = fmaf(dy[i], (x[i] - mean) * rstd, dg[i]);
+            db[i] += dy[i];
+        }
+    }
+    const int64_t D = (int64_t)a.units * N;
+    float* to = a.partial + (int64_t)blockIdx.y * 2 * D + (int64_t)piece * N;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        to[i] = dg[i];
+        to[D + i] = db[i];
+    }
+}
+
+namespace {
+
+constexpr int kWidePieces = 256;             // longest row that lies in the registers of a wave: 4 pieces a lane
+constexpr int kBwdBlocks = 1024;             // workgroups (= partial rows) of a large backward pass
+constexpr int kWideChunks = 64;              // row chunks of the wide columns' sums
+
+// Lanes (G) and pieces a lane (P) of a row.
+int lanes_of(int units)
+{
+    int G = 4;
+    while (G < units && G < kWave) G *= 2;
+    return G;
+}
+
+// G, P of a row as constants: CALL(G, P)
+#define FS_DISPATCH_ROW(units, CALL)                                                    \
+    do {                                                                                \
+        if ((units) > 128) { CALL(64, 4); }                                             \
+        else if ((units) > 64) { CALL(64, 2); }                                         \
+        else switch (lanes_of(units)) {                                                 \
+            case 4: CALL(4, 1); break;                                                  \
+            case 8: CALL(8, 1); break;                                                  \
+            case 16: CALL(16, 1); break;                                                \
+            case 32: CALL(32, 1); break;                                                \
+            default: CALL(64, 1); break;                                                \
+        }                                                                               \
+    } while (0)
+
+constexpr int fwd_rows(int P) { return P == 1 ? 4 : P == 2 ? 2 : 1; }
+constexpr int bwd_rows(int P) { return P == 1 ? 2 : 1; }
+
+int64_t bwd_blocks(int64_t n, int units)
+{
+    if (units > kWidePieces) return n < kWideChunks ? n : kWideChunks;
+    const int P = units > 128 ? 4 : units > 64 ? 2 : 1;
+    const int64_t per = (int64_t)(kBlock / lanes_of(units)) * bwd_rows(P);
+    const int64_t need = (n + per - 1) / per;
+    return need < kBwdBlocks ? need : kBwdBlocks;
+}
+
+template <int DT>
+fs_status norm_fwd_launch(const NormArgs& a, hipStream_t s)
+{
+    const bool pack = a.codes != nullptr;
+    if (a.units > kWidePieces) {
+        if (pack) FS_LAUNCH("norm_fwd_wide", (norm_fwd_wide_kernel<DT, true>), dim3((unsigned)a.n), dim3(kBlock), s, a);
+        else FS_LAUNCH("norm_fwd_wide", (norm_fwd_wide_kernel<DT, false>), dim3((unsigned)a.n), dim3(kBlock), s, a);
+        return FS_OK;
+    }
+#define CALL(G, P)                                                                                                        \
+    do {                                                                                                                  \
+        constexpr int U = fwd_rows(P);                                                                                    \
+        const unsigned grid = (unsigned)((a.n + (kBlock / G) * U - 1) / ((kBlock / G) * U));                              \
+        if (pack) FS_LAUNCH("norm_fwd", (norm_fwd_kernel<DT, G, P, U, true>), dim3(grid), dim3(kBlock), s, a);            \
+        else FS_LAUNCH("norm_fwd", (norm_fwd_kernel<DT, G, P, U, false>), dim3(grid), dim3(kBlock), s, a);                \
+    } while (0)
+    FS_DISPATCH_ROW(a.units, CALL);
+#undef CALL
+    return FS_OK;
+}
+
+template <int DT, bool PACKED>
+fs_status norm_bwd_launch(const NormArgs& a, hipStream_t s)
+{
+    const unsigned blocks = (unsigned)bwd_blocks(a.n, a.units);
+    if (a.units > kWidePieces) {
+        FS_LAUNCH("norm_bwd_wide", (norm_bwd_wide_kernel<DT, PACKED>), dim3((unsigned)a.n), dim3(kBlock), s, a);
+        FS_LAUNCH("norm_cols_wide", (norm_cols_wide_kernel<DT, PACKED>), dim3((unsigned)((a.units + kBlock - 1) / kBlock), blocks),
+                  dim3(kBlock), s, a);
+        return FS_OK;
+    }
+#define CALL(G, P) FS_LAUNCH("norm_bwd", (norm_bwd_kernel<DT, G, P, bwd_rows(P), PACKED>), dim3(blocks), dim3(kBlock), s, a)
+    FS_DISPATCH_ROW(a.units, CALL);
+#undef CALL
+    return FS_OK;
+}
+
+fs_status norm_bwd(NormArgs a, bool packed, int32_t D, fs_dtype dtype, float* dgamma, float* dbeta, void* workspace,
+                   size_t* workspace_bytes, hipStream_t s)
+{
+    if (!workspace_bytes) return FS_ERR_NULL;
+    const fs_status st = check_seq_rows(a.n, D, dtype, &a.units);
+    if (st != FS_OK) return st;
+    Carver ws(workspace);
+    const int64_t blocks = bwd_blocks(a.n, a.units);
+    a.partial = ws.take<float>((size_t)blocks * 2 * (size_t)D);
+    if (!workspace) { *workspace_bytes = ws.used; return FS_OK; }
+    if (*workspace_bytes < ws.used || misaligned(workspace, 256)) return FS_ERR_WORKSPACE;
+    if (!a.gamma || !dgamma || !dbeta) return FS_ERR_NULL;
+    if (a.n > 0 && (!a.dy || !a.mean || !a.rstd || !a.dx || (packed ? !a.x_codes || !a.x_exps : !a.x))) return FS_ERR_NULL;
+    if (misaligned(a.dy, 16) || misaligned(a.x, 16) || misaligned(a.x_codes, codes_alignment(dtype)) || misaligned(a.dx, 16) ||
+        misaligned(a.gamma, 16) || misaligned(dgamma, 4) || misaligned(dbeta, 4) || misaligned(a.mean, 4) || misaligned(a.rstd, 4))
+        return FS_ERR_ALIGN;
+    a.nb = (int)pack_blocks(D);
+    a.inv_D = 1.0f / (float)D;
+    if (a.n > 0) {
+        fs_status rc = FS_OK;
+        if (packed) {
+#define CALL(DT) rc = norm_bwd_launch<DT, true>(a, s)
+            FS_DISPATCH_DTYPE(dtype, CALL)
+#undef CALL
+        } else {
+#define CALL(DT) rc = norm_bwd_launch<DT, false>(a, s)
+            FS_DISPATCH_DTYPE(dtype, CALL)
+#undef CALL
+        }
+        if (rc != FS_OK) return rc;
+    }
+    FS_LAUNCH("norm_grad_sum", norm_grad_sum_kernel, dim3((unsigned)((2 * (int64_t)D + kWave - 1) / kWave)),
+              dim3(kGradSumWaves * kWave), s, a.partial, blocks, (int64_t)D, dgamma, dbeta);
+    return FS_OK;
+}
+
+}  // namespace
+}  // namespace fs
+
+extern "C" fs_status fs_seq_norm_fwd(
+    const void* x, int64_t n, int32_t D, fs_dtype dtype, const float* gamma, const float* beta, float eps,
+    void* y, float* mean, float* rstd, int8_t* codes, uint8_t* exps, void* stream)
+{
+    using namespace fs;
+    NormArgs a = {};
+    const fs_status st = check_seq_rows(n, D, dtype, &a.units);
+    if (st != FS_OK) return st;
+    if (!(eps > 0.0f) || __builtin_isinf(eps)) return FS_ERR_CONFIG;
+    if (n == 0) return FS_OK;
+    if (!x || !gamma || !beta || !y) return FS_ERR_NULL;
+    if ((mean != nullptr) != (rstd != nullptr) || (codes != nullptr) != (exps != nullptr)) return FS_ERR_NULL;
+    if (misaligned(x, 16) || misaligned(y, 16) || misaligned(gamma, 16) || misaligned(beta, 16) || misaligned(codes, codes_alignment(dtype)) ||
+        misaligned(mean, 4) || misaligned(rstd, 4))
+        return FS_ERR_ALIGN;
+    a.x = static_cast<const u32x4*>(x); a.n = n;
+    a.nb = (int)pack_blocks(D);
+    a.inv_D = 1.0f / (float)D; a.eps = eps;
+    a.gamma = gamma; a.beta = beta;
+    a.y = static_cast<u32x4*>(y); a.mean = mean; a.rstd = rstd;
+    a.codes = reinterpret_cast<uint32_t*>(codes); a.exps = exps;
+#define CALL(DT) return norm_fwd_launch<DT>(a, static_cast<hipStream_t>(stream))
+    FS_DISPATCH_DTYPE(dtype, CALL)
+#undef CALL
+}
+
+extern "C" fs_status fs_seq_norm_bwd(
+    const void* dy, const void* x, const float* mean, const float* rstd, int64_t n, int32_t D, fs_dtype dtype,
+    const float* gamma, void* dx, float* dgamma, float* dbeta,
+    void* workspace, size_t* workspace_bytes, void* stream)
+{
+    using namespace fs;
+    NormArgs a = {};
+    a.dy = static_cast<const u32x4*>(dy); a.x = static_cast<const u32x4*>(x); a.n = n;
+    a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd); a.gamma = gamma; a.dx = static_cast<u32x4*>(dx);
+    return norm_bwd(a, false, D, dtype, dgamma, dbeta, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+extern "C" fs_status fs_seq_norm_bwd_packed(
+    const void* dy, const int8_t* codes, const uint8_t* exps, const float* mean, const float* rstd,
+    int64_t n, int32_t D, fs_dtype dtype, const float* gamma, void* dx, float* dgamma, float* dbeta,
+    void* workspace, size_t* workspace_bytes, void* stream)
+{
+    using namespace fs;
+    NormArgs a = {};
+    a.dy = static_cast<const u32x4*>(dy); a.n = n;
+    a.x_codes = reinterpret_cast<const uint32_t*>(codes); a.x_exps = exps;
+    a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd); a.gamma = gamma; a.dx = static_cast<u32x4*>(dx);
+    return norm_bwd(a, true, D, dtype, dgamma, dbeta, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}

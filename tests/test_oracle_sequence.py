@@ -1,0 +1,141 @@
+"""The 64-bit statement of the sequence operators (oracle/sequence.py) against torch's own layer norm and autograd in
+float64, finite differences, brute force over the checkpoint's codes, and the checkpoint format's host functions."""
+import os
+import shutil
+import subprocess
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import sequence as seq
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
+
+
+def test_codes_are_the_nearest_and_the_step_the_smallest():
+    rng = np.random.default_rng(1)
+    x = rng.standard_normal((40, 70)) * 10.0 ** rng.integers(-30, 30, (40, 1))
+    x[0] = 0
+    x[1, :32] = 127.5                                    # rounds to 128: the next step
+    x[2, :32] = np.nextafter(np.float32(127.5), np.float32(0))
+    codes, exps = seq.pack8(x)
+    back = seq.unpack8(codes, exps)
+    for i in range(40):
+        for b in range(3):
+            v, c, E = x[i, 32 * b:32 * b + 32], codes[i, 32 * b:32 * b + 32].astype(float), int(exps[i, b])
+            step = 2.0 ** (E - 133)
+            assert np.all(np.abs(v - c * step) <= 0.5 * step)
+            assert np.array_equal(back[i, 32 * b:32 * b + 32], c * step)
+            if E > 1:                                    # half the step would need a code past 127
+                assert np.round(np.abs(v).max() / (step / 2)) > 127
+    assert exps[1, 0] == exps[2, 0] + 1 and codes[1, 0] == 64 and codes[2, 0] == 127 and exps[0, 0] == 1
+
+
+def test_ties_and_non_finite_values():
+    x = np.zeros((3, 40), np.float32)
+    x[0, :6] = [64, 0.5, 1.5, -0.5, -1.5, 2.5]           # step 1: ties to even
+    x[1, 3], x[1, 4], x[1, 5], x[1, 6] = np.nan, np.inf, -np.inf, 7
+    x[2, 35] = np.finfo(np.float32).max
+    codes, exps = seq.pack8(x)
+    assert exps[0, 0] == 133 and codes[0, :6].tolist() == [64, 0, 2, 0, -2, 2]
+    assert exps[1].tolist() == [255, 1] and codes[1, 3:8].tolist() == [-128, 127, -127, 0, 0]
+    back = seq.unpack8(codes, exps)
+    assert np.isnan(back[1, 3]) and back[1, 4] == np.inf and back[1, 5] == -np.inf and back[1, 6] == 0
+    assert exps[2, 1] == 254 and codes[2, 35] == 127 and np.isfinite(back[2, 35])
+
+
+FORMAT = r"""
+#include "pack8.h"
+#include <cmath>
+#include <cstdio>
+#include <cstring>
+int main()
+{
+    for (uint64_t i = 0; i < 0x7F800000u; i += 251) {
+        for (uint64_t b : {i, (i & 0xFF800000u) + 0x7EFFFF, (i & 0xFF800000u) + 0x7F0000, (i & 0xFF800000u) + 0x7FFFFF}) {
+            const uint32_t bits = (uint32_t)b;
+            float top;
+            std::memcpy(&top, &bits, 4);
+            const int E = fs::pack_exponent(bits);
+            float step;
+            const uint32_t sb = fs::pack_step_bits(E);
+            std::memcpy(&step, &sb, 4);
+            if (E < 1 || E > 254 || step != std::ldexp(1.0, E - 133)) { std::printf("step %08x %d\n", bits, E); return 1; }
+            const double q = (double)top / step;
+            if (E < 254 && std::nearbyint(q) > 127) { std::printf("too small %08x\n", bits); return 1; }
+            if (E > 1 && std::nearbyint(2 * q) <= 127) { std::printf("too large %08x\n", bits); return 1; }
+        }
+    }
+    if (fs::pack_exponent(0x7F800000u) != 255 || fs::pack_exponent(0x7FC00000u) != 255 || fs::pack_exponent(0) != 1) return 1;
+    if (fs::pack_step_bits(0) != fs::pack_step_bits(1)) return 1;
+    std::printf("format ok\n");
+    return 0;
+}
+"""
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="g++ not found")
+def test_exponents_on_the_host(tmp_path):
+    src, exe = tmp_path / "driver.cpp", tmp_path / "driver"
+    src.write_text(FORMAT)
+    built = subprocess.run(["g++", "-std=c++17", "-O1", "-D__HIP_PLATFORM_AMD__", "-I" + os.path.join(ROCM, "include"),
+                            "-I" + os.path.join(ROOT, "include"), "-I" + os.path.join(ROOT, "paper_2301_02959_amd", "csrc"),
+                            str(src), "-o", str(exe)], capture_output=True, text=True)
+    assert built.returncode == 0, built.stderr[-2000:]
+    run = subprocess.run([str(exe)], capture_output=True, text=True, timeout=120)
+    assert run.returncode == 0 and "format ok" in run.stdout, run.stdout + run.stderr
+
+
+def test_norm_is_torchs_in_64_bits():
+    torch.manual_seed(3)
+    x = torch.randn(9, 24, dtype=torch.float64).mul_(3).add_(1).requires_grad_()
+    gamma, beta = torch.randn(24, dtype=torch.float64).requires_grad_(), torch.randn(24, dtype=torch.float64).requires_grad_()
+    dy = torch.randn(9, 24, dtype=torch.float64)
+    y = torch.nn.functional.layer_norm(x, (24,), gamma, beta, 1e-5)
+    y.backward(dy)
+    gy, mean, rstd = seq.norm_fwd(x.detach().numpy(), gamma.detach().numpy(), beta.detach().numpy(), 1e-5)
+    assert np.allclose(gy, y.detach().numpy(), atol=1e-12, rtol=0)
+    dx, dg, db = seq.norm_bwd(dy.numpy(), x.detach().numpy(), mean, rstd, gamma.detach().numpy())
+    for got, want in ((dx, x.grad), (dg, gamma.grad), (db, beta.grad)):
+        assert np.allclose(got, want.numpy(), atol=1e-12, rtol=0)
+
+
+def _scan_torch(x, gate, offsets, h0):
+    f = torch.sigmoid(gate)
+    h, last = [], []
+    for s in range(len(offsets) - 1):
+        v = h0[s]
+        for t in range(offsets[s], offsets[s + 1]):
+            v = f[t] * v + (1 - f[t]) * x[t]
+            h.append(v)
+        last.append(v)
+    return torch.stack(h), torch.stack(last)
+
+
+def test_recurrence_and_its_gradient():
+    torch.manual_seed(4)
+    offsets, D = [0, 3, 3, 4, 12, 12], 5
+    n, S = 12, 5
+    x, gate, dh = (torch.randn(n, D, dtype=torch.float64) for _ in range(3))
+    h0, dl = torch.randn(S, D, dtype=torch.float64), torch.randn(S, D, dtype=torch.float64)
+    leaves = [t.requires_grad_() for t in (x, gate, h0)]
+    h, last = _scan_torch(*leaves[:2], offsets, leaves[2])
+    ((h * dh).sum() + (last * dl).sum()).backward()
+    a = [t.detach().numpy() for t in (x, gate, h0)]
+    gh, glast, _, _ = seq.scan_fwd(a[0], a[1], offsets, a[2])
+    assert np.allclose(gh, h.detach().numpy(), atol=1e-12, rtol=0) and np.allclose(glast, last.detach().numpy(), atol=1e-12, rtol=0)
+    dx, dg, d0, _, _, _ = seq.scan_bwd(dh.numpy(), dl.numpy(), a[0], a[1], gh, offsets, a[2])
+    for got, leaf in ((dx, x), (dg, gate), (d0, h0)):
+        assert np.allclose(got, leaf.grad.numpy(), atol=1e-12, rtol=0)
+    # and against differences: the loss at both sides of each gate
+    def loss(gate_):
+        hh, ll, _, _ = seq.scan_fwd(a[0], gate_, offsets, a[2])
+        return (hh * dh.numpy()).sum() + (ll * dl.numpy()).sum()
+    for t, d in ((0, 0), (2, 4), (3, 1), (7, 2), (11, 3)):
+        up, down = a[1].copy(), a[1].copy()
+        up[t, d] += 1e-5
+        down[t, d] -= 1e-5
+        # central difference: off by step^2 / 6 times a third derivative below 1 here, and by 1e-16 / 1e-5
+        assert abs((loss(up) - loss(down)) / 2e-5 - dg[t, d]) < 1e-8
