@@ -355,9 +355,12 @@ def test_scan_gates_at_the_ends():
     off_d = torch.from_numpy(off).to(DEV)
     h, last = torch.empty_like(x), torch.empty(3, 64, device=DEV)
     fs.fs_seq_scan_fwd(x, gate, off_d, 1, 3, h0, h, last)
-    assert torch.equal(h[5], x[5]) and torch.equal(h[6], h[5]) and torch.equal(h[61], x[61]) and torch.equal(h[139], h[99])
+    assert torch.equal(h[5], x[5]) and torch.equal(h[6], h[5]) and torch.equal(h[61], x[61])
     assert torch.equal(h[152], x[152])
+    # rows 100 .. 139 keep row 99's state; bit for bit only where it reaches them row by row: a stretch of rows folded to v -> A v + B
+    # first hands on another rounding of the same number.  Both lie within the recurrence's bound of the exact state (1 + 1 of them apart).
     wh, wl, bh, bl = seq.scan_fwd(host(x), np.clip(host(gate), -1000, 1000), off, host(h0))
+    assert np.all(np.abs(host(h[139]) - host(h[99])) <= bh[139] + bh[99] + 2 * half_step(torch.float32, wh[99]))
     inside(h, wh, half_step(torch.float32, wh) + bh)
     dx, dg, d0 = torch.empty_like(x), torch.empty_like(x), torch.empty(3, 64, device=DEV)
     fs.fs_seq_scan_bwd(dh, dl, x, gate, h_in, off_d, 1, 3, h0, dx, dg, d0)
