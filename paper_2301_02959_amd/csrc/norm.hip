@@ -217,9 +217,7 @@ struct XPiece {
     __device__ __forceinline__ void values(float* v) const
     {
         if constexpr (PACKED) {
-            const float step = __uint_as_float(pack_step_bits((int)raw[2]));
-            unpack_four(raw[0], (int)raw[2], step, v);
-            if constexpr (Piece<DT>::N == 8) unpack_four(raw[1], (int)raw[2], step, v + 4);
+            unpack_piece<Piece<DT>::N>(raw[0], raw[1], (int)raw[2], v);
         } else {
             Piece<DT>::unpack(raw, v);
         }

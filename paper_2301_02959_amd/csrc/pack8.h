@@ -50,20 +50,42 @@ __device__ __forceinline__ uint32_t pack_four(const float* v, int E)
 {
     int c[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) c[i] = E == kPackLost ? pack_code_lost(v[i]) : pack_code(v[i], E);
+    for (int i = 0; i < 4; ++i) c[i] = pack_code(v[i], E);
+    if (ballot(E == kPackLost) != 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[i] = E == kPackLost ? pack_code_lost(v[i]) : c[i];
+    }
     return (uint32_t)(c[0] & 255) | (uint32_t)(c[1] & 255) << 8 | (uint32_t)(c[2] & 255) << 16 | (uint32_t)c[3] << 24;
 }
 
-// Four values from their codes; `step` = the block's step.
-__device__ __forceinline__ void unpack_four(uint32_t codes, int E, float step, float* v)
+// Four values from their codes: in a block of finite values, in one that keeps its infinities and NaN alone.
+__device__ __forceinline__ void unpack_four(uint32_t codes, float step, float* v)
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = (float)((int32_t)(codes << (24 - 8 * i)) >> 24) * step;
-    if (E == kPackLost) {
+}
+
+__device__ __forceinline__ void unpack_four_lost(uint32_t codes, float* v)
+{
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int c = (int32_t)(codes << (24 - 8 * i)) >> 24;
-            v[i] = __uint_as_float(c == -128 ? 0x7FC00000u : c == 0 ? 0u : c > 0 ? 0x7F800000u : 0xFF800000u);
+    for (int i = 0; i < 4; ++i) {
+        const int c = (int32_t)(codes << (24 - 8 * i)) >> 24;
+        v[i] = __uint_as_float(c == -128 ? 0x7FC00000u : c == 0 ? 0u : c > 0 ? 0x7F800000u : 0xFF800000u);
+    }
+}
+
+// The N values (4 or 8) of a piece from its codes.  A block with an infinity or a NaN is a branch of the wave: as a selection
+// a value it costs more than all the rest.
+template <int N>
+__device__ __forceinline__ void unpack_piece(uint32_t codes0, uint32_t codes1, int E, float* v)
+{
+    const float step = __uint_as_float(pack_step_bits(E));
+    unpack_four(codes0, step, v);
+    if constexpr (N == 8) unpack_four(codes1, step, v + 4);
+    if (ballot(E == kPackLost) != 0) {
+        if (E == kPackLost) {
+            unpack_four_lost(codes0, v);
+            if constexpr (N == 8) unpack_four_lost(codes1, v + 4);
         }
     }
 }

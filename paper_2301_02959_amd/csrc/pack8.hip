@@ -68,11 +68,9 @@ __global__ __launch_bounds__(kBlock) void unpack8_kernel(const uint32_t* __restr
     const PackPlace<LPB> p = pack_place<LPB>(n, nb, units);
     if (!p.in) return;
     const int E = exps[p.row * nb + p.block];
-    const float step = __uint_as_float(pack_step_bits(E));
     const uint32_t* from = codes + (p.row * units + p.piece) * (N / 4);
     float v[N];
-    unpack_four(from[0], E, step, v);
-    if constexpr (N == 8) unpack_four(from[1], E, step, v + 4);
+    unpack_piece<N>(from[0], N == 8 ? from[N / 8] : 0u, E, v);
     if constexpr (DT == FS_F16) {
         // 2^16 is a value of blocks with fp16's largest numbers in them; what was finite stays finite
         if (E != kPackLost) {

@@ -17,6 +17,8 @@
 // Tiles are handed out in their order by a counter, so the tiles that a workgroup waits for are running or done, and every
 // tile publishes whatever the data: every wait ends.  A published pair is one 8-byte word that is its own flag (relaxed
 // atomics at the scope of the GPU, nothing else is passed on), cleared by a launch in front.
+#include <type_traits>
+
 #include "pack8.h"
 #include "seq_rows.h"
 
@@ -45,45 +47,61 @@ struct ScanArgs {
     int64_t strides;                 // workgroups a block of columns; those past `tiles` only look after empty sequences
     int col_blocks;                  // blocks of G pieces of columns
     uint64_t* words;                 // [tiles][col_blocks][G * N]
+    int32_t* tile_seq;               // [tiles]: the sequence that the row before the tile is in
     uint32_t* ticket;                // null: one tile, nothing to wait for
 };
 
 // f and 1 - f of a gate, each to the precision of e^-gate (1 - f is not taken from f, which is 1 for large gates).
 __device__ __forceinline__ void gate_pair(float gate, float* f, float* o)
 {
-    const float e = __expf(-gate);
+    const float e = __builtin_amdgcn_exp2f(gate * -1.44269504f);
     *f = __builtin_amdgcn_rcpf(1.0f + e);
     *o = e > 1e30f ? 1.0f : e * *f;                     // e = infinity (a shut gate): f = 0, 1 - f = 1
 }
 
-// One of the three saved inputs of the backward pass at a row's piece, from the rows or from their checkpoint; 0: x, 1: gate, 2: h.
+// p[at] by an offset of 32 bits in bytes (kMostPieces keeps them in range): a scalar base and one vector register.
+template <typename T>
+__device__ __forceinline__ T* piece_at(T* p, uint32_t at)
+{
+    using Byte = typename std::conditional<std::is_const<T>::value, const char, char>::type;
+    return reinterpret_cast<T*>(reinterpret_cast<Byte*>(p) + (uint32_t)(at * sizeof(T)));
+}
+
+// The same number, of which the compiler does not know that it has it already: it is worked out again where it is needed
+// instead of kept in a register over the whole kernel (or, with no register left, in scratch memory, whose loads wait for
+// the stores in flight: 9 % of the forward pass).
+__device__ __forceinline__ uint32_t again(uint32_t v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// One of the three saved inputs of the backward pass (0: x, 1: gate, 2: h) at a row's piece, from the rows or from their
+// checkpoint.  base: a row, the same for the whole workgroup; at: row - base in pieces, plus the piece; block: row - base in
+// blocks of columns, plus the block.
 template <int DT, bool PACKED, int WHICH>
 struct Saved {
     u32x4 raw;                       // PACKED: the codes in [0], [1]; the exponent in [2]
-    __device__ __forceinline__ void zero() { raw = u32x4{0u, 0u, 0u, 0u}; }
-    __device__ __forceinline__ void load(const ScanArgs& a, int64_t row, int piece)
+    __device__ __forceinline__ void load(const ScanArgs& a, int64_t base, uint32_t at, uint32_t block)
     {
-        constexpr int N = Piece<DT>::N, LPB = kPackBlock / N;
+        constexpr int N = Piece<DT>::N;
         if constexpr (PACKED) {
-            const uint32_t* from = a.codes[WHICH] + (row * a.units + piece) * (N / 4);
             if constexpr (N == 8) {
-                const u32x2 c = *reinterpret_cast<const u32x2*>(from);
+                const u32x2 c = load_stream(piece_at(reinterpret_cast<const u32x2*>(a.codes[WHICH]) + base * a.units, at));
                 raw[0] = c[0]; raw[1] = c[1];
             } else {
-                raw[0] = *from;
+                raw[0] = load_stream(piece_at(a.codes[WHICH] + base * a.units, at));
             }
-            raw[2] = a.exps[WHICH][row * a.nb + piece / LPB];
+            raw[2] = (a.exps[WHICH] + base * a.nb)[block];
         } else {
             const u32x4* from = WHICH == 0 ? a.x : WHICH == 1 ? a.gate : a.h_in;
-            raw = from[row * a.units + piece];
+            raw = load_stream(piece_at(from + base * a.units, at));
         }
     }
     __device__ __forceinline__ void values(float* v) const
     {
         if constexpr (PACKED) {
-            const float step = __uint_as_float(pack_step_bits((int)raw[2]));
-            unpack_four(raw[0], (int)raw[2], step, v);
-            if constexpr (Piece<DT>::N == 8) unpack_four(raw[1], (int)raw[2], step, v + 4);
+            unpack_piece<Piece<DT>::N>(raw[0], raw[1], (int)raw[2], v);
         } else {
             Piece<DT>::unpack(raw, v);
         }
@@ -113,32 +131,40 @@ struct ScanShared {
     uint32_t ticket;
 };
 
-// Marks the first and last rows of the sequences in tile `row0` ..  Every thread calls it; contains barriers.  With bad
-// offsets the marks are arbitrary but inside the tile.
+// Marks the first and last rows of the sequences in tile `row0` ..; the first wave does it, `s` = the sequence that row
+// row0 - 1 is in.  With bad offsets the marks are arbitrary but inside the tile.
 template <class Shape>
-__device__ __forceinline__ void mark_sequences(const ScanArgs& a, int64_t row0, ScanShared<Shape>* sh)
+__device__ __forceinline__ void mark_sequences(const ScanArgs& a, int64_t row0, int s0, ScanShared<Shape>* sh)
 {
-    for (int w = threadIdx.x; w < Shape::T / 32; w += kBlock) sh->firsts[w] = sh->lasts[w] = 0u;
-    const int64_t row1 = row0 + Shape::T < a.n ? row0 + Shape::T : a.n;
-    // the sequence that row0 - 1 is in and those after it, as far as they begin before row1
-    int64_t s = row0 == 0 ? 0 : wave_table_of(a.offsets, (int)a.S, 1, row0 - 1);
-    s += threadIdx.x;
-    __syncthreads();
-    for (bool more = true; more; s += kBlock) {
-        int64_t b = row1, e = row1;
-        if (s < a.S) { b = a.offsets[s]; e = a.offsets[s + 1]; }
+    const int lane = lane_id();
+    for (int w = lane; w < Shape::T / 32; w += kWave) sh->firsts[w] = sh->lasts[w] = 0u;
+    const int rows = a.n - row0 < Shape::T ? (int)(a.n - row0) : Shape::T;
+    int64_t s = (int64_t)s0 + lane;
+    for (bool more = true; more; s += kWave) {
+        int64_t b = rows, e = rows;                     // from row0 on
+        if (s < a.S) { b = a.offsets[s] - row0; e = a.offsets[s + 1] - row0; }
         if (b < e) {
-            if (b >= row0 && b < row1) {
-                atomicOr(&sh->firsts[(b - row0) >> 5], 1u << ((b - row0) & 31));
-                sh->first_of[b - row0] = (int32_t)s;
+            if (b >= 0 && b < rows) {
+                const int at = (int)b;
+                atomicOr(&sh->firsts[at >> 5], 1u << (at & 31));
+                sh->first_of[at] = (int32_t)s;
             }
-            if (e > row0 && e <= row1) {
-                atomicOr(&sh->lasts[(e - 1 - row0) >> 5], 1u << ((e - 1 - row0) & 31));
-                sh->last_of[e - 1 - row0] = (int32_t)s;
+            if (e > 0 && e <= rows) {
+                const int at = (int)e - 1;
+                atomicOr(&sh->lasts[at >> 5], 1u << (at & 31));
+                sh->last_of[at] = (int32_t)s;
             }
         }
-        more = __syncthreads_or(threadIdx.x == kBlock - 1 && s < a.S && b < row1) != 0;
+        more = (ballot(b < rows) >> (kWave - 1)) != 0;  // the last lane's is still in the tile
     }
+}
+
+// Sequence to begin with in tile k of the rows; the workgroup's first wave calls it.
+__device__ __forceinline__ int first_sequence(const ScanArgs& a, int64_t tile)
+{
+    if (a.tile_seq == nullptr) return 0;
+    const int s = a.tile_seq[tile];
+    return s < 0 ? 0 : s;                               // (at most S - 1, and sequences from S on are not looked at)
 }
 
 // Marks of a group's R rows, bit r for row r.
@@ -147,6 +173,22 @@ __device__ __forceinline__ uint32_t group_marks(const uint32_t* marks, int group
 {
     const int at = group * Shape::R;
     return (marks[at >> 5] >> (at & 31)) & (uint32_t)((1ull << Shape::R) - 1ull);
+}
+
+// Bit q: group q has a mark.  The same in every lane, so it is kept in scalar registers.
+template <class Shape>
+__device__ __forceinline__ uint64_t marked_groups(const uint32_t* marks)
+{
+    constexpr int kPer = 32 / Shape::R;                 // groups to a word
+    uint64_t groups = 0;
+#pragma unroll
+    for (int w = 0; w < Shape::T / 32; ++w) {
+        const uint32_t m = (uint32_t)__builtin_amdgcn_readfirstlane((int)marks[w]);
+#pragma unroll
+        for (int g = 0; g < kPer; ++g)
+            if ((m >> (g * Shape::R)) & (uint32_t)((1ull << Shape::R) - 1ull)) groups |= 1ull << (w * kPer + g);
+    }
+    return groups;
 }
 
 constexpr uint64_t kNotReady = ~0ull;
@@ -293,8 +335,39 @@ __device__ __forceinline__ void store_state(float* p, int64_t at, const float* v
     for (int i = 0; i < N; i += 4) *reinterpret_cast<f32x4*>(p + at + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
 }
 
+// Where a lane's rows lie, as 32-bit offsets from the tile's first row.  Rows past n and pieces past the row's end are
+// replaced by ones that are there: loads without a predicate go out one after the other, predicated ones wait for each
+// other.  What is computed from the replacements is not stored and reaches no row that is.
+template <class Shape>
+struct Place {
+    int group, piece, rows;          // rows: of the group's R, those before n (none: not positive)
+    bool in;                         // the piece is in the row
+    int64_t row0;
+    uint32_t units, own, first;      // in pieces; own: the piece, or one that is there; first: the group's first row's
+    __device__ __forceinline__ Place(const ScanArgs& a, int64_t tile, int cb)
+    {
+        group = threadIdx.x / Shape::G;
+        piece = cb * Shape::G + (int)(threadIdx.x % Shape::G);
+        in = piece < a.units;
+        row0 = tile * Shape::T;
+        const int64_t left = a.n - row0;
+        rows = (left < Shape::T ? (int)left : Shape::T) - group * Shape::R;
+        units = (uint32_t)a.units;
+        own = in ? (uint32_t)piece : units - 1u;
+        first = (uint32_t)(group * Shape::R) * units + own;
+    }
+    __device__ __forceinline__ uint32_t at(int r) const { return r < rows ? first + r * units : own; }
+    __device__ __forceinline__ uint32_t row(int r) const { return r < rows ? (uint32_t)(group * Shape::R + r) : 0u; }
+    // place of the lane's columns in the states of sequence s
+    __device__ __forceinline__ int64_t state(const ScanArgs& a, int32_t s) const
+    {
+        return ((int64_t)s * a.units + again((uint32_t)piece)) * Shape::N;
+    }
+    __device__ __forceinline__ bool stored(int r) const { return in && r < rows; }
+};
+
 template <int DT, int G, int R>
-__global__ __launch_bounds__(kBlock, 4) void scan_fwd_kernel(ScanArgs a)
+__global__ __launch_bounds__(kBlock, 3) void scan_fwd_kernel(ScanArgs a)
 {
     using Shape = ScanShape<DT, G, R>;
     constexpr int N = Shape::N;
@@ -303,23 +376,20 @@ __global__ __launch_bounds__(kBlock, 4) void scan_fwd_kernel(ScanArgs a)
     const int64_t k = t / (uint32_t)a.col_blocks;
     const int cb = (int)(t % (uint32_t)a.col_blocks);
     if (k < a.tiles) {
-        const int lig = threadIdx.x % G, group = threadIdx.x / G;
-        const int piece = cb * G + lig;
-        const bool in = piece < a.units;
-        const int64_t row0 = k * Shape::T, first = row0 + group * R;
-        const int64_t cols = (int64_t)a.units * N, col = (int64_t)piece * N;
+        const Place<Shape> p(a, k, cb);
+        const int lig = threadIdx.x % G;
+        const u32x4* from_x = a.x + p.row0 * a.units;
+        const u32x4* from_g = a.gate + p.row0 * a.units;
         u32x4 raw_x[R], raw_g[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            raw_x[r] = raw_g[r] = u32x4{0u, 0u, 0u, 0u};
-            if (in && first + r < a.n) {
-                raw_g[r] = load_stream(a.gate + (first + r) * a.units + piece);
-                raw_x[r] = load_stream(a.x + (first + r) * a.units + piece);
-            }
+            raw_g[r] = load_stream(piece_at(from_g, p.at(r)));
+            raw_x[r] = load_stream(piece_at(from_x, p.at(r)));
         }
-        mark_sequences(a, row0, &sh);
-        uint32_t firsts = group_marks<Shape>(sh.firsts, group);
-        const uint32_t lasts = group_marks<Shape>(sh.lasts, group);
+        if (wave_id() == 0) mark_sequences<Shape>(a, p.row0, first_sequence(a, k), &sh);
+        __syncthreads();
+        const uint32_t firsts = group_marks<Shape>(sh.firsts, p.group);
+        const uint32_t lasts = group_marks<Shape>(sh.lasts, p.group);
         float f[R][N], b[R][N];
         float A[N], B[N];
 #pragma unroll
@@ -335,15 +405,16 @@ __global__ __launch_bounds__(kBlock, 4) void scan_fwd_kernel(ScanArgs a)
                 gate_pair(f[r][i], &f[r][i], &o);
                 b[r][i] = o * x[i];
             }
-            if ((firsts >> r) & 1) {
-                if (a.ends_in != nullptr && in) {
+            const bool begins = (firsts >> r) & 1;
+            if (ballot(begins) != 0) {                  // (few rows: a branch of the wave, not a selection a value)
+                if (begins && a.ends_in != nullptr && p.in) {
                     float h0[N];
-                    load_state<N>(a.ends_in, (int64_t)sh.first_of[group * R + r] * cols + col, h0);
+                    load_state<N>(a.ends_in, p.state(a, sh.first_of[p.group * R + r]), h0);
 #pragma unroll
                     for (int i = 0; i < N; ++i) b[r][i] = fmaf(f[r][i], h0[i], b[r][i]);
                 }
 #pragma unroll
-                for (int i = 0; i < N; ++i) B[i] = 0.0f;                // nothing of the sequence before, a NaN either
+                for (int i = 0; i < N; ++i) B[i] = begins ? 0.0f : B[i];        // nothing of the sequence before, a NaN either
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -351,67 +422,61 @@ __global__ __launch_bounds__(kBlock, 4) void scan_fwd_kernel(ScanArgs a)
                 B[i] = fmaf(f[r][i], B[i], b[r][i]);
             }
         }
-        store_state<N>(&sh.A[group][0], lig * N, A);
-        store_state<N>(&sh.B[group][0], lig * N, B);
+        store_state<N>(&sh.A[p.group][0], lig * N, A);
+        store_state<N>(&sh.B[p.group][0], lig * N, B);
         __syncthreads();
-        uint64_t resets = 0;
-        for (int q = 0; q < Shape::Q; ++q) resets |= (uint64_t)(group_marks<Shape>(sh.firsts, q) != 0) << q;
         const bool open = k > 0 && !(sh.firsts[0] & 1u);
-        carry_states<Shape>(a, k, cb, resets, open, &sh);
+        carry_states<Shape>(a, k, cb, marked_groups<Shape>(sh.firsts), open, &sh);
         float h[N];
+        u32x4* to = a.h + p.row0 * a.units;
+        const uint32_t first = again(p.first);
 #pragma unroll
-        for (int i = 0; i < N; ++i) h[i] = sh.B[group][lig * N + i];
+        for (int i = 0; i < N; ++i) h[i] = sh.B[p.group][lig * N + i];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            if ((firsts >> r) & 1) {
+            const bool begins = (firsts >> r) & 1;
+            if (ballot(begins) != 0) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) h[i] = 0.0f;
+                for (int i = 0; i < N; ++i) h[i] = begins ? 0.0f : h[i];
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) h[i] = fmaf(f[r][i], h[i], b[r][i]);
-            if (in && first + r < a.n) {
-                store_stream(a.h + (first + r) * a.units + piece, Piece<DT>::pack(h));
-                if (((lasts >> r) & 1) && a.ends_out != nullptr) store_state<N>(a.ends_out, (int64_t)sh.last_of[group * R + r] * cols + col, h);
-            }
+            if (p.stored(r)) store_stream(piece_at(to, first + r * p.units), Piece<DT>::pack(h));
+            if (a.ends_out != nullptr && ((lasts >> r) & 1) && p.in) store_state<N>(a.ends_out, p.state(a, sh.last_of[p.group * R + r]), h);
         }
     }
     empty_sequences<Shape>(a, k, cb);
 }
 
 template <int DT, int G, int R, bool PACKED>
-__global__ __launch_bounds__(kBlock, 2) void scan_bwd_kernel(ScanArgs a)
+__global__ __launch_bounds__(kBlock, DT == FS_F32 && !PACKED ? 2 : 3) void scan_bwd_kernel(ScanArgs a)
 {
     using Shape = ScanShape<DT, G, R>;
-    constexpr int N = Shape::N, Q = Shape::Q;
+    constexpr int N = Shape::N, Q = Shape::Q, LPB = kPackBlock / N;
     __shared__ ScanShared<Shape> sh;
     const uint32_t t = take_ticket(a, &sh);
     const int64_t k = t / (uint32_t)a.col_blocks;       // from the batch's end
     const int cb = (int)(t % (uint32_t)a.col_blocks);
     if (k < a.tiles) {
-        const int lig = threadIdx.x % G, group = threadIdx.x / G, q = Q - 1 - group;
-        const int piece = cb * G + lig;
-        const bool in = piece < a.units;
-        const int64_t row0 = (a.tiles - 1 - k) * Shape::T, first = row0 + group * R;
-        const int64_t cols = (int64_t)a.units * N, col = (int64_t)piece * N;
+        const Place<Shape> p(a, a.tiles - 1 - k, cb);
+        const int lig = threadIdx.x % G, q = Q - 1 - p.group;
+        const u32x4* from_d = a.dh + p.row0 * a.units;
         u32x4 raw_d[R];
         Saved<DT, PACKED, 0> x[R];
         Saved<DT, PACKED, 1> gate[R];
         Saved<DT, PACKED, 2> before[R];                 // h of the row before
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            raw_d[r] = u32x4{0u, 0u, 0u, 0u};
-            gate[r].zero();
-            x[r].zero();
-            before[r].zero();
-            if (in && first + r < a.n) {
-                gate[r].load(a, first + r, piece);
-                raw_d[r] = load_stream(a.dh + (first + r) * a.units + piece);
-                x[r].load(a, first + r, piece);
-                if (first + r > 0) before[r].load(a, first + r - 1, piece);
-            }
+            const uint32_t row = p.row(r), at = p.at(r), block = row * (uint32_t)a.nb + p.own / LPB;
+            gate[r].load(a, p.row0, at, block);
+            raw_d[r] = load_stream(piece_at(from_d, at));
+            x[r].load(a, p.row0, at, block);
+            const uint32_t up = p.row0 > 0 || row == 0 ? 0u : 1u;               // the batch's first row stands in for the one before it
+            before[r].load(a, p.row0 > 0 ? p.row0 - 1 : 0, at - up * p.units, block - up * (uint32_t)a.nb);
         }
-        mark_sequences(a, row0, &sh);
-        const uint32_t firsts = group_marks<Shape>(sh.firsts, group), lasts = group_marks<Shape>(sh.lasts, group);
+        if (wave_id() == 0) mark_sequences<Shape>(a, p.row0, first_sequence(a, a.tiles - 1 - k), &sh);
+        __syncthreads();
+        const uint32_t firsts = group_marks<Shape>(sh.firsts, p.group), lasts = group_marks<Shape>(sh.lasts, p.group);
         float f[R][N], o[R][N], d[R][N];
         float A[N], B[N];
 #pragma unroll
@@ -422,15 +487,16 @@ __global__ __launch_bounds__(kBlock, 2) void scan_bwd_kernel(ScanArgs a)
             Piece<DT>::unpack(raw_d[r], d[r]);
 #pragma unroll
             for (int i = 0; i < N; ++i) gate_pair(f[r][i], &f[r][i], &o[r][i]);
-            if ((lasts >> r) & 1) {
-                if (a.ends_in != nullptr && in) {
+            const bool ends = (lasts >> r) & 1;
+            if (ballot(ends) != 0) {
+                if (ends && a.ends_in != nullptr && p.in) {
                     float end[N];
-                    load_state<N>(a.ends_in, (int64_t)sh.last_of[group * R + r] * cols + col, end);
+                    load_state<N>(a.ends_in, p.state(a, sh.last_of[p.group * R + r]), end);
 #pragma unroll
                     for (int i = 0; i < N; ++i) d[r][i] += end[i];
                 }
 #pragma unroll
-                for (int i = 0; i < N; ++i) B[i] = 0.0f;
+                for (int i = 0; i < N; ++i) B[i] = ends ? 0.0f : B[i];
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -441,26 +507,30 @@ __global__ __launch_bounds__(kBlock, 2) void scan_bwd_kernel(ScanArgs a)
         store_state<N>(&sh.A[q][0], lig * N, A);
         store_state<N>(&sh.B[q][0], lig * N, B);
         __syncthreads();
-        uint64_t resets = 0;
-        for (int j = 0; j < Q; ++j) resets |= (uint64_t)(group_marks<Shape>(sh.lasts, Q - 1 - j) != 0) << j;
+        // the groups in the order of the walk: from the last
+        const uint64_t resets = __builtin_bitreverse64(marked_groups<Shape>(sh.lasts)) >> (64 - Q);
         const bool open = k > 0 && !(sh.lasts[Shape::T / 32 - 1] >> 31);
         carry_states<Shape>(a, k, cb, resets, open, &sh);
         float U[N];
+        u32x4* to_x = a.dx + p.row0 * a.units;
+        u32x4* to_g = a.dgate + p.row0 * a.units;
+        const uint32_t first = again(p.first);
 #pragma unroll
         for (int i = 0; i < N; ++i) U[i] = sh.B[q][lig * N + i];
 #pragma unroll
         for (int r = R - 1; r >= 0; --r) {
-            if ((lasts >> r) & 1) {
-#pragma unroll
-                for (int i = 0; i < N; ++i) U[i] = 0.0f;
-            }
             float xv[N], hb[N], dx[N], dg[N];
             x[r].values(xv);
             before[r].values(hb);
-            if ((firsts >> r) & 1) {
+            const bool ends = (lasts >> r) & 1, begins = (firsts >> r) & 1;
+            if (ballot(ends) != 0) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) hb[i] = 0.0f;
-                if (a.h0 != nullptr && in) load_state<N>(a.h0, (int64_t)sh.first_of[group * R + r] * cols + col, hb);
+                for (int i = 0; i < N; ++i) U[i] = ends ? 0.0f : U[i];
+            }
+            if (ballot(begins) != 0) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) hb[i] = begins ? 0.0f : hb[i];
+                if (begins && a.h0 != nullptr && p.in) load_state<N>(a.h0, p.state(a, sh.first_of[p.group * R + r]), hb);
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -469,22 +539,31 @@ __global__ __launch_bounds__(kBlock, 2) void scan_bwd_kernel(ScanArgs a)
                 dg[i] = dx[i] * f[r][i] * (hb[i] - xv[i]);
                 U[i] = f[r][i] * Gi;
             }
-            if (in && first + r < a.n) {
-                store_stream(a.dx + (first + r) * a.units + piece, Piece<DT>::pack(dx));
-                store_stream(a.dgate + (first + r) * a.units + piece, Piece<DT>::pack(dg));
-                if (((firsts >> r) & 1) && a.ends_out != nullptr) store_state<N>(a.ends_out, (int64_t)sh.first_of[group * R + r] * cols + col, U);
+            if (p.stored(r)) {
+                store_stream(piece_at(to_x, first + r * p.units), Piece<DT>::pack(dx));
+                store_stream(piece_at(to_g, first + r * p.units), Piece<DT>::pack(dg));
             }
+            if (a.ends_out != nullptr && begins && p.in) store_state<N>(a.ends_out, p.state(a, sh.first_of[p.group * R + r]), U);
         }
     }
     empty_sequences<Shape>(a, k, cb);
 }
 
-// All words not ready, no ticket taken.
-__global__ __launch_bounds__(kBlock) void scan_clear_kernel(u32x4* __restrict__ words, int64_t pieces, uint32_t* __restrict__ ticket)
+// All words not ready, no ticket taken, and every tile's first sequence: the largest s with offsets[s] <= the row before it
+// (bad offsets: some s in [0, S)).  A thread a tile bisects here, beside the writes of the others; in the tiles' own workgroups
+// the search is a chain of loads in front of everything.
+__global__ __launch_bounds__(kBlock) void scan_clear_kernel(ScanArgs a, int64_t pieces, int tile_rows)
 {
     const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (i < pieces) words[i] = u32x4{~0u, ~0u, ~0u, ~0u};
-    if (i == 0) *ticket = 0u;
+    if (i < pieces) reinterpret_cast<u32x4*>(a.words)[i] = u32x4{~0u, ~0u, ~0u, ~0u};
+    if (i == 0) *a.ticket = 0u;
+    if (i >= a.tiles) return;
+    int64_t lo = 0, hi = a.S;                            // offsets[lo] <= i * tile_rows - 1 (taken as given for lo = 0) < offsets[hi]
+    while (hi - lo > 1) {
+        const int64_t mid = lo + ((hi - lo) >> 1);
+        if (a.offsets[mid] < i * tile_rows) lo = mid; else hi = mid;
+    }
+    a.tile_seq[i] = (int32_t)lo;
 }
 
 // One token of every session: a 16-byte piece of x, gate and out to a lane, its states as fp32 beside it.
@@ -525,8 +604,11 @@ int scan_lanes(int units)
     return (units + 15) / 16 * 16 <= (units + 7) / 8 * 8 ? 16 : 8;
 }
 
+// Longest row, in 16-byte pieces (4 MB): a tile of at most 1024 rows is addressed by 32-bit offsets in bytes.
+constexpr int kMostPieces = (1 << 18) - 1;
+
 // Values of a lane: R rows of a 16-byte piece.
-constexpr int kFwdValues = 32, kBwdValues = 32;
+constexpr int kFwdValues = 64, kBwdValues = 32;
 
 // Everything that follows from the sizes; *a gets them, `words` the workspace's places.
 fs_status plan_scan(int64_t n, int32_t D, fs_dtype dtype, int32_t T, int32_t B, int values, Carver* ws, ScanArgs* a, int* lanes)
@@ -534,6 +616,7 @@ fs_status plan_scan(int64_t n, int32_t D, fs_dtype dtype, int32_t T, int32_t B, 
     const fs_status st = check_seq_rows(n, D, dtype, &a->units);
     if (st != FS_OK) return st;
     if (T < 1 || B < 1 || (int64_t)T * B >= (1LL << 31)) return FS_ERR_SIZE;
+    if (a->units > kMostPieces) return FS_ERR_SIZE;
     a->S = (int64_t)T * B;
     a->n = n;
     a->nb = (int)pack_blocks(D);
@@ -547,18 +630,19 @@ fs_status plan_scan(int64_t n, int32_t D, fs_dtype dtype, int32_t T, int32_t B, 
     if (a->strides * a->col_blocks > 0x7FFFFFFF) return FS_ERR_SIZE;
     if (a->tiles > 1) {
         a->words = ws->take<uint64_t>((size_t)a->tiles * (size_t)a->col_blocks * (size_t)(*lanes * N));
+        a->tile_seq = ws->take<int32_t>((size_t)a->tiles);
         a->ticket = ws->take<uint32_t>(1);
     }
     return FS_OK;
 }
 
-fs_status clear_words(const ScanArgs& a, int columns, hipStream_t s)
+fs_status clear_words(const ScanArgs& a, int columns, int values, hipStream_t s)
 {
     if (a.tiles <= 1) return FS_OK;
-    const int64_t pieces = a.tiles * a.col_blocks * columns / 2;
+    const int64_t pieces = a.tiles * a.col_blocks * columns / 2;            // at least 8 a tile
     const int64_t grid = (pieces + kBlock - 1) / kBlock;
     if (grid > 0x7FFFFFFF) return FS_ERR_SIZE;
-    FS_LAUNCH("scan_clear", scan_clear_kernel, dim3((unsigned)grid), dim3(kBlock), s, reinterpret_cast<u32x4*>(a.words), pieces, a.ticket);
+    FS_LAUNCH("scan_clear", scan_clear_kernel, dim3((unsigned)grid), dim3(kBlock), s, a, pieces, kBlock * values / columns);
     return FS_OK;
 }
 
@@ -611,7 +695,7 @@ fs_status scan_bwd(ScanArgs a, bool packed, int32_t D, fs_dtype dtype, int32_t T
         misaligned(a.codes[2], codes_alignment(dtype)) || misaligned(a.h0, 16) || misaligned(a.ends_in, 16) ||
         misaligned(a.ends_out, 16) || misaligned(a.offsets, 8))
         return FS_ERR_ALIGN;
-    st = clear_words(a, lanes * (dtype == FS_F32 ? 4 : 8), s);
+    st = clear_words(a, lanes * (dtype == FS_F32 ? 4 : 8), kBwdValues, s);
     if (st != FS_OK) return st;
     if (packed) {
 #define CALL(DT) st = scan_bwd_launch<DT, true>(a, lanes, s)
@@ -648,7 +732,7 @@ extern "C" fs_status fs_seq_scan_fwd(
     a.x = static_cast<const u32x4*>(x); a.gate = static_cast<const u32x4*>(gate);
     a.offsets = offsets; a.ends_in = h0; a.h = static_cast<u32x4*>(h); a.ends_out = h_last; a.status = dev_status;
     hipStream_t hs = static_cast<hipStream_t>(stream);
-    st = clear_words(a, lanes * (dtype == FS_F32 ? 4 : 8), hs);
+    st = clear_words(a, lanes * (dtype == FS_F32 ? 4 : 8), kFwdValues, hs);
     if (st != FS_OK) return st;
 #define CALL(DT) return scan_fwd_launch<DT>(a, lanes, hs)
     FS_DISPATCH_DTYPE(dtype, CALL)
