@@ -131,40 +131,50 @@ struct ScanShared {
     uint32_t ticket;
 };
 
-// Marks the first and last rows of the sequences in tile `row0` ..; the first wave does it, `s` = the sequence that row
-// row0 - 1 is in.  With bad offsets the marks are arbitrary but inside the tile.
+// The bounds of the 64 sequences from the one on that the row before the tile is in, one a lane of the first wave.  Loaded in
+// front of the rows: loads come back in their order, and behind the rows the marks would wait for all of them.
+struct Bounds {
+    int64_t s, b, e;
+    __device__ __forceinline__ void load(const ScanArgs& a)
+    {
+        b = e = a.n;
+        if (s < a.S) { b = a.offsets[s]; e = a.offsets[s + 1]; }
+    }
+    __device__ __forceinline__ Bounds(const ScanArgs& a, int s0)
+    {
+        s = (int64_t)(s0 < 0 ? 0 : s0) + lane_id();     // (s0 is at most S - 1)
+        load(a);
+    }
+};
+
+// Marks the first and last rows of the sequences in the tile from row0 on; the first wave does it.  With bad offsets the marks
+// are arbitrary but inside the tile.
 template <class Shape>
-__device__ __forceinline__ void mark_sequences(const ScanArgs& a, int64_t row0, int s0, ScanShared<Shape>* sh)
+__device__ __forceinline__ void mark_sequences(const ScanArgs& a, int64_t row0, Bounds seqs, ScanShared<Shape>* sh)
 {
     const int lane = lane_id();
     for (int w = lane; w < Shape::T / 32; w += kWave) sh->firsts[w] = sh->lasts[w] = 0u;
     const int rows = a.n - row0 < Shape::T ? (int)(a.n - row0) : Shape::T;
-    int64_t s = (int64_t)s0 + lane;
-    for (bool more = true; more; s += kWave) {
-        int64_t b = rows, e = rows;                     // from row0 on
-        if (s < a.S) { b = a.offsets[s] - row0; e = a.offsets[s + 1] - row0; }
+    const auto mark = [&] {
+        const int64_t b = seqs.b - row0, e = seqs.e - row0;
         if (b < e) {
             if (b >= 0 && b < rows) {
                 const int at = (int)b;
                 atomicOr(&sh->firsts[at >> 5], 1u << (at & 31));
-                sh->first_of[at] = (int32_t)s;
+                sh->first_of[at] = (int32_t)seqs.s;
             }
             if (e > 0 && e <= rows) {
                 const int at = (int)e - 1;
                 atomicOr(&sh->lasts[at >> 5], 1u << (at & 31));
-                sh->last_of[at] = (int32_t)s;
+                sh->last_of[at] = (int32_t)seqs.s;
             }
         }
-        more = (ballot(b < rows) >> (kWave - 1)) != 0;  // the last lane's is still in the tile
+        return (ballot(b < rows && seqs.s < a.S) >> (kWave - 1)) != 0;          // the last lane's begins in the tile or before it
+    };
+    for (bool more = mark(); more; more = mark()) {
+        seqs.s += kWave;
+        seqs.load(a);
     }
-}
-
-// Sequence to begin with in tile k of the rows; the workgroup's first wave calls it.
-__device__ __forceinline__ int first_sequence(const ScanArgs& a, int64_t tile)
-{
-    if (a.tile_seq == nullptr) return 0;
-    const int s = a.tile_seq[tile];
-    return s < 0 ? 0 : s;                               // (at most S - 1, and sequences from S on are not looked at)
 }
 
 // Marks of a group's R rows, bit r for row r.
@@ -312,7 +322,7 @@ __device__ __forceinline__ uint32_t take_ticket(const ScanArgs& a, ScanShared<Sh
     if (a.ticket == nullptr) return blockIdx.x;
     if (threadIdx.x == 0) sh->ticket = atomicAdd(a.ticket, 1u);
     __syncthreads();
-    return sh->ticket;
+    return (uint32_t)__builtin_amdgcn_readfirstlane((int)sh->ticket);       // scalar, and so are the addresses made of it
 }
 
 __device__ __forceinline__ void load_four(const float* p, int64_t at, float* v)
@@ -367,7 +377,7 @@ struct Place {
 };
 
 template <int DT, int G, int R>
-__global__ __launch_bounds__(kBlock, 3) void scan_fwd_kernel(ScanArgs a)
+__global__ __launch_bounds__(kBlock, 3) void scan_fwd_kernel(ScanArgs a, const int32_t* __restrict__ tile_seq)
 {
     using Shape = ScanShape<DT, G, R>;
     constexpr int N = Shape::N;
@@ -378,6 +388,7 @@ __global__ __launch_bounds__(kBlock, 3) void scan_fwd_kernel(ScanArgs a)
     if (k < a.tiles) {
         const Place<Shape> p(a, k, cb);
         const int lig = threadIdx.x % G;
+        const Bounds bounds(a, tile_seq == nullptr ? 0 : tile_seq[k]);          // (in every wave: without a branch it goes out first)
         const u32x4* from_x = a.x + p.row0 * a.units;
         const u32x4* from_g = a.gate + p.row0 * a.units;
         u32x4 raw_x[R], raw_g[R];
@@ -386,7 +397,7 @@ __global__ __launch_bounds__(kBlock, 3) void scan_fwd_kernel(ScanArgs a)
             raw_g[r] = load_stream(piece_at(from_g, p.at(r)));
             raw_x[r] = load_stream(piece_at(from_x, p.at(r)));
         }
-        if (wave_id() == 0) mark_sequences<Shape>(a, p.row0, first_sequence(a, k), &sh);
+        if (wave_id() == 0) mark_sequences<Shape>(a, p.row0, bounds, &sh);
         __syncthreads();
         const uint32_t firsts = group_marks<Shape>(sh.firsts, p.group);
         const uint32_t lasts = group_marks<Shape>(sh.lasts, p.group);
@@ -449,7 +460,7 @@ __global__ __launch_bounds__(kBlock, 3) void scan_fwd_kernel(ScanArgs a)
 }
 
 template <int DT, int G, int R, bool PACKED>
-__global__ __launch_bounds__(kBlock, DT == FS_F32 && !PACKED ? 2 : 3) void scan_bwd_kernel(ScanArgs a)
+__global__ __launch_bounds__(kBlock, DT == FS_F32 && !PACKED ? 2 : 3) void scan_bwd_kernel(ScanArgs a, const int32_t* __restrict__ tile_seq)
 {
     using Shape = ScanShape<DT, G, R>;
     constexpr int N = Shape::N, Q = Shape::Q, LPB = kPackBlock / N;
@@ -460,21 +471,26 @@ __global__ __launch_bounds__(kBlock, DT == FS_F32 && !PACKED ? 2 : 3) void scan_
     if (k < a.tiles) {
         const Place<Shape> p(a, a.tiles - 1 - k, cb);
         const int lig = threadIdx.x % G, q = Q - 1 - p.group;
+        const Bounds bounds(a, tile_seq == nullptr ? 0 : tile_seq[a.tiles - 1 - k]);
         const u32x4* from_d = a.dh + p.row0 * a.units;
         u32x4 raw_d[R];
         Saved<DT, PACKED, 0> x[R];
         Saved<DT, PACKED, 1> gate[R];
         Saved<DT, PACKED, 2> before[R];                 // h of the row before
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const uint32_t row = p.row(r), at = p.at(r), block = row * (uint32_t)a.nb + p.own / LPB;
-            gate[r].load(a, p.row0, at, block);
-            raw_d[r] = load_stream(piece_at(from_d, at));
-            x[r].load(a, p.row0, at, block);
-            const uint32_t up = p.row0 > 0 || row == 0 ? 0u : 1u;               // the batch's first row stands in for the one before it
-            before[r].load(a, p.row0 > 0 ? p.row0 - 1 : 0, at - up * p.units, block - up * (uint32_t)a.nb);
+        for (int r = R - 1; r >= 0; --r) {              // in the order of their use
+            const uint32_t block = p.row(r) * (uint32_t)a.nb + p.own / LPB;
+            gate[r].load(a, p.row0, p.at(r), block);
+            raw_d[r] = load_stream(piece_at(from_d, p.at(r)));
         }
-        if (wave_id() == 0) mark_sequences<Shape>(a, p.row0, first_sequence(a, a.tiles - 1 - k), &sh);
+#pragma unroll
+        for (int r = R - 1; r >= 0; --r) {
+            const uint32_t row = p.row(r), block = row * (uint32_t)a.nb + p.own / LPB;
+            x[r].load(a, p.row0, p.at(r), block);
+            const uint32_t up = p.row0 > 0 || row == 0 ? 0u : 1u;               // the batch's first row stands in for the one before it
+            before[r].load(a, p.row0 > 0 ? p.row0 - 1 : 0, p.at(r) - up * p.units, block - up * (uint32_t)a.nb);
+        }
+        if (wave_id() == 0) mark_sequences<Shape>(a, p.row0, bounds, &sh);
         __syncthreads();
         const uint32_t firsts = group_marks<Shape>(sh.firsts, p.group), lasts = group_marks<Shape>(sh.lasts, p.group);
         float f[R][N], o[R][N], d[R][N];
@@ -657,7 +673,7 @@ template <int DT>
 fs_status scan_fwd_launch(const ScanArgs& a, int lanes, hipStream_t s)
 {
     const dim3 grid((unsigned)(a.strides * a.col_blocks));
-#define CALL(G) FS_LAUNCH("scan_fwd", (scan_fwd_kernel<DT, G, kFwdValues / Piece<DT>::N>), grid, dim3(kBlock), s, a)
+#define CALL(G) FS_LAUNCH("scan_fwd", (scan_fwd_kernel<DT, G, kFwdValues / Piece<DT>::N>), grid, dim3(kBlock), s, a, a.tile_seq)
     FS_DISPATCH_LANES(lanes, CALL)
 #undef CALL
     return FS_OK;
@@ -667,7 +683,7 @@ template <int DT, bool PACKED>
 fs_status scan_bwd_launch(const ScanArgs& a, int lanes, hipStream_t s)
 {
     const dim3 grid((unsigned)(a.strides * a.col_blocks));
-#define CALL(G) FS_LAUNCH("scan_bwd", (scan_bwd_kernel<DT, G, kBwdValues / Piece<DT>::N, PACKED>), grid, dim3(kBlock), s, a)
+#define CALL(G) FS_LAUNCH("scan_bwd", (scan_bwd_kernel<DT, G, kBwdValues / Piece<DT>::N, PACKED>), grid, dim3(kBlock), s, a, a.tile_seq)
     FS_DISPATCH_LANES(lanes, CALL)
 #undef CALL
     return FS_OK;
