@@ -45,7 +45,9 @@ struct ScanArgs {
     int32_t* status;
     int64_t tiles;
     int64_t strides;                 // workgroups a block of columns; those past `tiles` only look after empty sequences
-    int col_blocks;                  // blocks of G pieces of columns
+    int col_blocks;                  // blocks of `lanes` pieces of columns
+    int lanes, groups;               // of a workgroup
+    int by_lanes, by_columns;        // t / lanes and t / (columns of a workgroup) as (t * this) >> 16, t <= kBlock
     uint64_t* words;                 // [tiles][col_blocks][G * N]
     int32_t* tile_seq;               // [tiles]: the sequence that the row before the tile is in
     uint32_t* ticket;                // null: one tile, nothing to wait for
@@ -59,14 +61,6 @@ __device__ __forceinline__ void gate_pair(float gate, float* f, float* o)
     *o = e > 1e30f ? 1.0f : e * *f;                     // e = infinity (a shut gate): f = 0, 1 - f = 1
 }
 
-// p[at] by an offset of 32 bits in bytes (kMostPieces keeps them in range): a scalar base and one vector register.
-template <typename T>
-__device__ __forceinline__ T* piece_at(T* p, uint32_t at)
-{
-    using Byte = typename std::conditional<std::is_const<T>::value, const char, char>::type;
-    return reinterpret_cast<T*>(reinterpret_cast<Byte*>(p) + (uint32_t)(at * sizeof(T)));
-}
-
 // The same number, of which the compiler does not know that it has it already: it is worked out again where it is needed
 // instead of kept in a register over the whole kernel (or, with no register left, in scratch memory, whose loads wait for
 // the stores in flight: 9 % of the forward pass).
@@ -76,10 +70,34 @@ __device__ __forceinline__ uint32_t again(uint32_t v)
     return v;
 }
 
+// p[at] by an offset of 32 bits in bytes (kMostPieces keeps them in range): a scalar base and one vector register.
+template <typename T>
+__device__ __forceinline__ T* piece_at(T* p, uint32_t at)
+{
+    using Byte = typename std::conditional<std::is_const<T>::value, const char, char>::type;
+    return reinterpret_cast<T*>(reinterpret_cast<Byte*>(p) + (uint32_t)(at * sizeof(T)));
+}
+
+// Rows of whole cache lines are read once by one instruction each and streamed past the caches; of other rows a line belongs
+// to two, and to instructions apart in time, so they go through the caches (us, streamed : cached: 4.2 M rows of 256 bytes
+// forward 620 : 653, backward 1217 : 1301; of 272 bytes forward 769 : 753; of 48 bytes backward 557 : 412).
+template <bool STREAM, typename T>
+__device__ __forceinline__ T load_rows(const T* p)
+{
+    if constexpr (STREAM) return load_stream(p);
+    else return *p;
+}
+template <bool STREAM, typename T>
+__device__ __forceinline__ void store_rows(T* p, T v)
+{
+    if constexpr (STREAM) store_stream(p, v);
+    else *p = v;
+}
+
 // One of the three saved inputs of the backward pass (0: x, 1: gate, 2: h) at a row's piece, from the rows or from their
 // checkpoint.  base: a row, the same for the whole workgroup; at: row - base in pieces, plus the piece; block: row - base in
 // blocks of columns, plus the block.
-template <int DT, bool PACKED, int WHICH>
+template <int DT, bool PACKED, int WHICH, bool STREAM>
 struct Saved {
     u32x4 raw;                       // PACKED: the codes in [0], [1]; the exponent in [2]
     __device__ __forceinline__ void load(const ScanArgs& a, int64_t base, uint32_t at, uint32_t block)
@@ -87,15 +105,15 @@ struct Saved {
         constexpr int N = Piece<DT>::N;
         if constexpr (PACKED) {
             if constexpr (N == 8) {
-                const u32x2 c = load_stream(piece_at(reinterpret_cast<const u32x2*>(a.codes[WHICH]) + base * a.units, at));
+                const u32x2 c = load_rows<STREAM>(piece_at(reinterpret_cast<const u32x2*>(a.codes[WHICH]) + base * a.units, at));
                 raw[0] = c[0]; raw[1] = c[1];
             } else {
-                raw[0] = load_stream(piece_at(a.codes[WHICH] + base * a.units, at));
+                raw[0] = load_rows<STREAM>(piece_at(a.codes[WHICH] + base * a.units, at));
             }
             raw[2] = (a.exps[WHICH] + base * a.nb)[block];
         } else {
             const u32x4* from = WHICH == 0 ? a.x : WHICH == 1 ? a.gate : a.h_in;
-            raw = load_stream(piece_at(from + base * a.units, at));
+            raw = load_rows<STREAM>(piece_at(from + base * a.units, at));
         }
     }
     __device__ __forceinline__ void values(float* v) const
@@ -108,26 +126,52 @@ struct Saved {
     }
 };
 
-// G lanes a row, R rows a group.
+// A workgroup's tile: G lanes a row and Q groups of R rows each.  G_ = 0: G is an argument.
 template <int DT, int G_, int R_>
 struct ScanShape {
-    static constexpr int N = Piece<DT>::N, G = G_, R = R_;
-    static constexpr int C = G * N;                     // columns of a workgroup
-    static constexpr int Q = kBlock / G;                // groups
-    static constexpr int T = Q * R;                     // rows of a tile
-    static constexpr int P = kBlock / C;                // threads a column
-    static_assert(T % 32 == 0 && 32 % R == 0 && C <= kBlock, "");
+    static constexpr int N = Piece<DT>::N, R = R_;
+    static constexpr int kMostGroups = 64, kMostRows = kMostGroups * R;
+    int G, Q;
+    int C;                           // columns of the workgroup, at most kBlock
+    int P;                           // threads a column
+    int T;                           // rows
+    int by_lanes, by_columns;        // (scalars all; the thread's places below are worked out where they are needed)
+    static_assert(32 % R == 0, "");
+    __device__ __forceinline__ explicit ScanShape(const ScanArgs& a)
+    {
+        if constexpr (G_ > 0) {
+            G = G_; Q = kBlock / G_; C = G_ * N; P = kBlock / (G_ * N);
+        } else {
+            G = a.lanes; Q = a.groups; C = G * N; P = (kBlock * a.by_columns) >> 16;
+            by_lanes = a.by_lanes; by_columns = a.by_columns;
+        }
+        T = Q * R;
+    }
+    // the thread's group (Q or more: none) and lane in it
+    __device__ __forceinline__ int group() const
+    {
+        if constexpr (G_ > 0) return (int)(again(threadIdx.x) / (uint32_t)G_);
+        return (int)(again(threadIdx.x) * (uint32_t)by_lanes) >> 16;
+    }
+    __device__ __forceinline__ int lane() const { return (int)threadIdx.x - group() * G; }
+    // which of the threads of its column it is (P: none), and the column
+    __device__ __forceinline__ int part() const
+    {
+        if constexpr (G_ > 0) return (int)(again(threadIdx.x) / (uint32_t)(G_ * N));
+        return (int)(again(threadIdx.x) * (uint32_t)by_columns) >> 16;
+    }
+    __device__ __forceinline__ int col() const { return (int)threadIdx.x - part() * C; }
 };
 
 constexpr int kLookAhead = 4;                           // tiles that a thread looks back over at once
 
 template <class Shape>
 struct ScanShared {
-    float A[Shape::Q][Shape::C];                        // the groups' pairs in the order of the walk; then B is what reaches them
-    float B[Shape::Q][Shape::C];
-    uint64_t seen[Shape::P * kLookAhead][Shape::C];     // the words of the tiles looked back over
-    uint32_t firsts[Shape::T / 32], lasts[Shape::T / 32];   // rows of the tile where a sequence begins, ends
-    int32_t first_of[Shape::T], last_of[Shape::T];      // ... and which one
+    float A[kBlock * Shape::N], B[kBlock * Shape::N];   // [Q][C] in the order of the walk: the groups' pairs, then what lies before each
+    uint64_t seen[kBlock * kLookAhead];                 // [P * kLookAhead][C]: the words of the tiles looked back over
+    float reaches[kBlock];                              // [C]: the state that reaches the tile
+    uint32_t firsts[Shape::kMostRows / 32], lasts[Shape::kMostRows / 32];       // rows of the tile where a sequence begins, ends
+    int32_t first_of[Shape::kMostRows], last_of[Shape::kMostRows];              // ... and which one
     uint32_t ticket;
 };
 
@@ -150,11 +194,11 @@ struct Bounds {
 // Marks the first and last rows of the sequences in the tile from row0 on; the first wave does it.  With bad offsets the marks
 // are arbitrary but inside the tile.
 template <class Shape>
-__device__ __forceinline__ void mark_sequences(const ScanArgs& a, int64_t row0, Bounds seqs, ScanShared<Shape>* sh)
+__device__ __forceinline__ void mark_sequences(const ScanArgs& a, const Shape& tile, int64_t row0, Bounds seqs, ScanShared<Shape>* sh)
 {
     const int lane = lane_id();
-    for (int w = lane; w < Shape::T / 32; w += kWave) sh->firsts[w] = sh->lasts[w] = 0u;
-    const int rows = a.n - row0 < Shape::T ? (int)(a.n - row0) : Shape::T;
+    if (lane < Shape::kMostRows / 32) sh->firsts[lane] = sh->lasts[lane] = 0u;
+    const int rows = a.n - row0 < tile.T ? (int)(a.n - row0) : tile.T;
     const auto mark = [&] {
         const int64_t b = seqs.b - row0, e = seqs.e - row0;
         if (b < e) {
@@ -177,28 +221,20 @@ __device__ __forceinline__ void mark_sequences(const ScanArgs& a, int64_t row0, 
     }
 }
 
-// Marks of a group's R rows, bit r for row r.
+// Marks of the thread's group, bit r for row r.
 template <class Shape>
-__device__ __forceinline__ uint32_t group_marks(const uint32_t* marks, int group)
+__device__ __forceinline__ uint32_t group_marks(const Shape& tile, const uint32_t* marks)
 {
-    const int at = group * Shape::R;
-    return (marks[at >> 5] >> (at & 31)) & (uint32_t)((1ull << Shape::R) - 1ull);
+    const int group = tile.group(), at = group * Shape::R;
+    return group < tile.Q ? (marks[at >> 5] >> (at & 31)) & (uint32_t)((1ull << Shape::R) - 1ull) : 0u;
 }
 
-// Bit q: group q has a mark.  The same in every lane, so it is kept in scalar registers.
 template <class Shape>
-__device__ __forceinline__ uint64_t marked_groups(const uint32_t* marks)
+__device__ __forceinline__ bool any_marks(const Shape& tile, const uint32_t* marks)
 {
-    constexpr int kPer = 32 / Shape::R;                 // groups to a word
-    uint64_t groups = 0;
-#pragma unroll
-    for (int w = 0; w < Shape::T / 32; ++w) {
-        const uint32_t m = (uint32_t)__builtin_amdgcn_readfirstlane((int)marks[w]);
-#pragma unroll
-        for (int g = 0; g < kPer; ++g)
-            if ((m >> (g * Shape::R)) & (uint32_t)((1ull << Shape::R) - 1ull)) groups |= 1ull << (w * kPer + g);
-    }
-    return groups;
+    uint32_t any = 0;
+    for (int w = 0; w * 32 < tile.T; ++w) any |= marks[w];
+    return __builtin_amdgcn_readfirstlane((int)any) != 0;
 }
 
 constexpr uint64_t kNotReady = ~0ull;
@@ -213,35 +249,48 @@ __device__ __forceinline__ bool is_state(uint64_t word) { return (uint32_t)(word
 
 __device__ __forceinline__ uint64_t state_word(float v) { return ((uint64_t)kIsState << 32) | __float_as_uint(v); }
 
-// From the groups' pairs in sh->A and sh->B to the states that reach the groups, in sh->B.  k: the tile's number in the order
-// of the walk; resets: bit q = a sequence begins in group q (in that order); open: the tile's first row goes on with a
+// A < 0 in a pair stands for a stretch in which a sequence begins: B is the state after it, whatever comes before.
+__device__ __forceinline__ bool begins_in(float A) { return (int32_t)__float_as_uint(A) < 0; }
+constexpr float kBegins = -1.0f;
+
+// The state after the stretch (A, B) where v is the one before it.  (A NaN's sign may be set; its B is a NaN too.)
+__device__ __forceinline__ float after(float A, float B, float v) { return begins_in(A) ? B : fmaf(A, v, B); }
+
+// From the groups' pairs in sh->A and sh->B to the pair of all that lies before each group in the tile, there, and the states
+// that reach the tile, in sh->reaches.  k: the tile's number in the order of the walk; known: a sequence begins in the tile
+// or with it, so the state after it does not depend on what comes before; open: the tile's first row goes on with a
 // sequence of the tile before.  Every thread calls it; contains barriers.
 template <class Shape>
-__device__ __forceinline__ void carry_states(const ScanArgs& a, int64_t k, int cb, uint64_t resets, bool open, ScanShared<Shape>* sh)
+__device__ __forceinline__ void carry_states(const ScanArgs& a, const Shape& tile, int64_t k, int cb, bool known, bool open, ScanShared<Shape>* sh)
 {
-    constexpr int C = Shape::C, Q = Shape::Q, P = Shape::P;
-    const int c = threadIdx.x % C, part = threadIdx.x / C;
+    const int C = tile.C, c = tile.col(), part = tile.part();
+    uint64_t* words = a.words + cb * C + c;
+    const int64_t stride = (int64_t)a.col_blocks * C;   // words of a tile
     float A = 1.0f, B = 0.0f;
-    if (a.ticket != nullptr) {
-        uint64_t* word = a.words + (k * a.col_blocks + cb) * C + c;
-        const bool known = resets != 0 || !open;        // the state after the tile does not depend on what comes before
-        if (part == 0) {
+    if (part == 0) {
 #pragma unroll 8
-            for (int q = 0; q < Q; ++q) {
-                const float qA = sh->A[q][c], qB = sh->B[q][c];
-                const bool reset = (resets >> q) & 1;
-                B = reset ? qB : fmaf(qA, B, qB);
-                A *= qA;
-            }
-            __hip_atomic_store(word, known ? state_word(B) : pair_word(A, B), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        for (int q = 0; q < tile.Q; ++q) {
+            const float qA = sh->A[q * C + c], qB = sh->B[q * C + c];
+            sh->A[q * C + c] = A;
+            sh->B[q * C + c] = B;
+            B = after(qA, qB, B);
+            A = begins_in(qA) ? kBegins : A * qA;
         }
-        float v = 0.0f;                                 // the state that reaches the tile
-        if (open) {
-            const auto look = [&](int64_t p) {
-                return p < 0 ? state_word(0.0f)
-                             : __hip_atomic_load(a.words + (p * a.col_blocks + cb) * C + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            };
-            const auto look_back = [&](int64_t nearest) {   // a window of tiles nearest, nearest - 1, ... into LDS, all ready
+        if (a.ticket != nullptr)
+            __hip_atomic_store(words + k * stride, known ? state_word(B) : pair_word(A, B), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    float v = 0.0f;                                     // the state that reaches the tile
+    if (open) {
+        const int W = tile.P * kLookAhead;
+        const auto look = [&](int64_t p) {
+            return p < 0 ? state_word(0.0f) : __hip_atomic_load(words + p * stride, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        };
+        // back, window by window of W tiles, until there is a state in every column; then forward again from there
+        int64_t window = 0;
+        bool back = true;
+        for (;;) {
+            const int64_t nearest = k - 1 - window * W;
+            if (part < tile.P) {
                 uint64_t seen[kLookAhead];
 #pragma unroll
                 for (int u = 0; u < kLookAhead; ++u) seen[u] = look(nearest - part * kLookAhead - u);
@@ -251,53 +300,68 @@ __device__ __forceinline__ void carry_states(const ScanArgs& a, int64_t k, int c
                         __builtin_amdgcn_s_sleep(1);
                         seen[u] = look(nearest - part * kLookAhead - u);
                     }
-                    sh->seen[part * kLookAhead + u][c] = seen[u];
+                    sh->seen[(part * kLookAhead + u) * C + c] = seen[u];
                 }
-                __syncthreads();
-            };
-            // back, window by window, until there is a state in every column; then forward again from there
-            constexpr int W = P * kLookAhead;
-            int64_t window = 0;
-            for (bool all = false; !all; ++window) {
-                look_back(k - 1 - window * W);
+            }
+            __syncthreads();
+            if (back) {
                 bool found = part != 0;
-                for (int i = 0; i < W && !found; ++i) found = is_state(sh->seen[i][c]);
-                all = __syncthreads_and(found) != 0;
-            }
-            for (--window;;) {
-                if (part == 0) {
-#pragma unroll
-                    for (int i = W - 1; i >= 0; --i) {
-                        const uint64_t w = sh->seen[i][c];
-                        v = is_state(w) ? __uint_as_float((uint32_t)w) : fmaf(__uint_as_float((uint32_t)(w >> 32)), v, __uint_as_float((uint32_t)w));
-                    }
+                for (int i = 0; i < W && !found; ++i) found = is_state(sh->seen[i * C + c]);
+                if (__syncthreads_and(found) == 0) {
+                    ++window;
+                    continue;
                 }
-                if (window == 0) break;
-                __syncthreads();
-                look_back(k - 1 - --window * W);
+                back = false;
             }
+            if (part == 0) {
+#pragma unroll 4
+                for (int i = W - 1; i >= 0; --i) {
+                    const uint64_t w = sh->seen[i * C + c];
+                    const float wB = __uint_as_float((uint32_t)w);
+                    v = is_state(w) ? wB : fmaf(__uint_as_float((uint32_t)(w >> 32)), v, wB);
+                }
+            }
+            if (window == 0) break;
+            --window;
+            __syncthreads();
         }
         if (part == 0 && !known)
-            __hip_atomic_store(word, state_word(fmaf(A, v, B)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        B = v;
+            __hip_atomic_store(words + k * stride, state_word(fmaf(A, v, B)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    if (part == 0) {
-#pragma unroll 8
-        for (int q = 0; q < Q; ++q) {
-            const float qA = sh->A[q][c], qB = sh->B[q][c];
-            sh->B[q][c] = B;
-            B = ((resets >> q) & 1) ? qB : fmaf(qA, B, qB);
-        }
-    }
+    if (part == 0) sh->reaches[c] = v;
     __syncthreads();
+}
+
+// The states that reach the thread's group, q-th in the order of the walk.
+template <class Shape>
+__device__ __forceinline__ void group_states(const Shape& tile, int q, const ScanShared<Shape>& sh, float* v)
+{
+    constexpr int N = Shape::N;
+    const int c = tile.lane() * N, at = (tile.group() < tile.Q ? q : 0) * tile.C + c;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = after(sh.A[at + i], sh.B[at + i], sh.reaches[c + i]);
+}
+
+// The thread's pair into its place.
+template <class Shape>
+__device__ __forceinline__ void store_pair(const Shape& tile, int q, bool begins, const float* A, const float* B, ScanShared<Shape>* sh)
+{
+    constexpr int N = Shape::N;
+    if (tile.group() >= tile.Q) return;
+    const int at = q * tile.C + tile.lane() * N;
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        *reinterpret_cast<f32x4*>(&sh->A[at + i]) = begins ? f32x4{kBegins, kBegins, kBegins, kBegins} : f32x4{A[i], A[i + 1], A[i + 2], A[i + 3]};
+        *reinterpret_cast<f32x4*>(&sh->B[at + i]) = f32x4{B[i], B[i + 1], B[i + 2], B[i + 3]};
+    }
 }
 
 // The states of empty sequences pass through, and the offsets are looked over: 256 sequences at a time, dealt to the workgroups.
 template <class Shape>
-__device__ __forceinline__ void empty_sequences(const ScanArgs& a, int64_t k, int cb)
+__device__ __forceinline__ void empty_sequences(const ScanArgs& a, const Shape& tile, int64_t k, int cb)
 {
     const int64_t cols = (int64_t)a.units * Shape::N;
-    const int col = cb * Shape::C + 4 * lane_id();
+    const int col = cb * tile.C + 4 * lane_id();
     for (int64_t s0 = k * kBlock; s0 < a.S; s0 += a.strides * kBlock) {
         const int64_t s = s0 + threadIdx.x;
         bool empty = false;
@@ -309,7 +373,7 @@ __device__ __forceinline__ void empty_sequences(const ScanArgs& a, int64_t k, in
         if (a.ends_out == nullptr) continue;
         for (uint64_t left = ballot(empty); left != 0; left &= left - 1) {
             const int64_t at = (s0 + (threadIdx.x & ~(kWave - 1)) + __builtin_ctzll(left)) * cols + col;
-            if (4 * lane_id() < Shape::C && col < cols)
+            if (4 * lane_id() < tile.C && col < cols)
                 *reinterpret_cast<f32x4*>(a.ends_out + at) = a.ends_in ? *reinterpret_cast<const f32x4*>(a.ends_in + at) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
     }
@@ -350,31 +414,35 @@ __device__ __forceinline__ void store_state(float* p, int64_t at, const float* v
 // other.  What is computed from the replacements is not stored and reaches no row that is.
 template <class Shape>
 struct Place {
-    int group, piece, rows;          // rows: of the group's R, those before n (none: not positive)
+    int piece, rows;                 // rows: of the group's R, those before n (none: not positive)
+    uint32_t row_at;                 // the group's first row
     bool in;                         // the piece is in the row
     int64_t row0;
     uint32_t units, own, first;      // in pieces; own: the piece, or one that is there; first: the group's first row's
-    __device__ __forceinline__ Place(const ScanArgs& a, int64_t tile, int cb)
+    __device__ __forceinline__ Place(const ScanArgs& a, const Shape& tile, int64_t number, int cb)
     {
-        group = threadIdx.x / Shape::G;
-        piece = cb * Shape::G + (int)(threadIdx.x % Shape::G);
+        piece = cb * tile.G + tile.lane();
         in = piece < a.units;
-        row0 = tile * Shape::T;
+        row0 = number * tile.T;
+        row_at = (uint32_t)(tile.group() * Shape::R);
         const int64_t left = a.n - row0;
-        rows = (left < Shape::T ? (int)left : Shape::T) - group * Shape::R;
+        rows = (left < tile.T ? (int)left : tile.T) - (int)row_at;
         units = (uint32_t)a.units;
         own = in ? (uint32_t)piece : units - 1u;
-        first = (uint32_t)(group * Shape::R) * units + own;
+        first = row_at * units + own;
     }
     __device__ __forceinline__ uint32_t at(int r) const { return r < rows ? first + r * units : own; }
-    __device__ __forceinline__ uint32_t row(int r) const { return r < rows ? (uint32_t)(group * Shape::R + r) : 0u; }
-    // place of the lane's columns in the states of sequence s
-    __device__ __forceinline__ int64_t state(const ScanArgs& a, int32_t s) const
-    {
-        return ((int64_t)s * a.units + again((uint32_t)piece)) * Shape::N;
-    }
+    __device__ __forceinline__ uint32_t row(int r) const { return r < rows ? row_at + r : 0u; }
     __device__ __forceinline__ bool stored(int r) const { return in && r < rows; }
 };
+
+// The lane's columns in the states of sequence `which[row]` of the tile's row r of the thread's group; -1: it has none.
+template <class Shape>
+__device__ __forceinline__ int64_t state_at(const ScanArgs& a, const Shape& tile, int cb, const int32_t* which, int r)
+{
+    const int group = tile.group(), piece = cb * tile.G + (int)threadIdx.x - group * tile.G;
+    return piece < a.units ? ((int64_t)which[group * Shape::R + r] * a.units + piece) * Shape::N : -1;
+}
 
 template <int DT, int G, int R>
 __global__ __launch_bounds__(kBlock, 3) void scan_fwd_kernel(ScanArgs a, const int32_t* __restrict__ tile_seq)
@@ -382,25 +450,25 @@ __global__ __launch_bounds__(kBlock, 3) void scan_fwd_kernel(ScanArgs a, const i
     using Shape = ScanShape<DT, G, R>;
     constexpr int N = Shape::N;
     __shared__ ScanShared<Shape> sh;
+    const Shape tile(a);
     const uint32_t t = take_ticket(a, &sh);
     const int64_t k = t / (uint32_t)a.col_blocks;
     const int cb = (int)(t % (uint32_t)a.col_blocks);
     if (k < a.tiles) {
-        const Place<Shape> p(a, k, cb);
-        const int lig = threadIdx.x % G;
+        const Place<Shape> p(a, tile, k, cb);
         const Bounds bounds(a, tile_seq == nullptr ? 0 : tile_seq[k]);          // (in every wave: without a branch it goes out first)
         const u32x4* from_x = a.x + p.row0 * a.units;
         const u32x4* from_g = a.gate + p.row0 * a.units;
         u32x4 raw_x[R], raw_g[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            raw_g[r] = load_stream(piece_at(from_g, p.at(r)));
-            raw_x[r] = load_stream(piece_at(from_x, p.at(r)));
+            raw_g[r] = load_rows<(G > 0)>(piece_at(from_g, p.at(r)));
+            raw_x[r] = load_rows<(G > 0)>(piece_at(from_x, p.at(r)));
         }
-        if (wave_id() == 0) mark_sequences<Shape>(a, p.row0, bounds, &sh);
+        if (wave_id() == 0) mark_sequences(a, tile, p.row0, bounds, &sh);
         __syncthreads();
-        const uint32_t firsts = group_marks<Shape>(sh.firsts, p.group);
-        const uint32_t lasts = group_marks<Shape>(sh.lasts, p.group);
+        const uint32_t firsts = group_marks(tile, sh.firsts);
+        const uint32_t lasts = group_marks(tile, sh.lasts);
         float f[R][N], b[R][N];
         float A[N], B[N];
 #pragma unroll
@@ -418,11 +486,14 @@ __global__ __launch_bounds__(kBlock, 3) void scan_fwd_kernel(ScanArgs a, const i
             }
             const bool begins = (firsts >> r) & 1;
             if (ballot(begins) != 0) {                  // (few rows: a branch of the wave, not a selection a value)
-                if (begins && a.ends_in != nullptr && p.in) {
-                    float h0[N];
-                    load_state<N>(a.ends_in, p.state(a, sh.first_of[p.group * R + r]), h0);
+                if (begins && a.ends_in != nullptr) {
+                    const int64_t at = state_at(a, tile, cb, sh.first_of, r);
+                    if (at >= 0) {
+                        float h0[N];
+                        load_state<N>(a.ends_in, at, h0);
 #pragma unroll
-                    for (int i = 0; i < N; ++i) b[r][i] = fmaf(f[r][i], h0[i], b[r][i]);
+                        for (int i = 0; i < N; ++i) b[r][i] = fmaf(f[r][i], h0[i], b[r][i]);
+                    }
                 }
 #pragma unroll
                 for (int i = 0; i < N; ++i) B[i] = begins ? 0.0f : B[i];        // nothing of the sequence before, a NaN either
@@ -433,16 +504,14 @@ __global__ __launch_bounds__(kBlock, 3) void scan_fwd_kernel(ScanArgs a, const i
                 B[i] = fmaf(f[r][i], B[i], b[r][i]);
             }
         }
-        store_state<N>(&sh.A[p.group][0], lig * N, A);
-        store_state<N>(&sh.B[p.group][0], lig * N, B);
+        store_pair(tile, tile.group(), firsts != 0, A, B, &sh);
         __syncthreads();
-        const bool open = k > 0 && !(sh.firsts[0] & 1u);
-        carry_states<Shape>(a, k, cb, marked_groups<Shape>(sh.firsts), open, &sh);
+        const bool open = k > 0 && !(__builtin_amdgcn_readfirstlane((int)sh.firsts[0]) & 1);
+        carry_states(a, tile, k, cb, k == 0 || any_marks(tile, sh.firsts), open, &sh);
         float h[N];
-        u32x4* to = a.h + p.row0 * a.units;
-        const uint32_t first = again(p.first);
-#pragma unroll
-        for (int i = 0; i < N; ++i) h[i] = sh.B[p.group][lig * N + i];
+        const Place<Shape> out(a, tile, k, cb);
+        u32x4* to = a.h + out.row0 * a.units;
+        group_states(tile, tile.group(), sh, h);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const bool begins = (firsts >> r) & 1;
@@ -452,36 +521,39 @@ __global__ __launch_bounds__(kBlock, 3) void scan_fwd_kernel(ScanArgs a, const i
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) h[i] = fmaf(f[r][i], h[i], b[r][i]);
-            if (p.stored(r)) store_stream(piece_at(to, first + r * p.units), Piece<DT>::pack(h));
-            if (a.ends_out != nullptr && ((lasts >> r) & 1) && p.in) store_state<N>(a.ends_out, p.state(a, sh.last_of[p.group * R + r]), h);
+            if (out.stored(r)) store_rows<(G > 0)>(piece_at(to, out.first + r * out.units), Piece<DT>::pack(h));
+            if (a.ends_out != nullptr && ((lasts >> r) & 1)) {
+                const int64_t at = state_at(a, tile, cb, sh.last_of, r);
+                if (at >= 0) store_state<N>(a.ends_out, at, h);
+            }
         }
     }
-    empty_sequences<Shape>(a, k, cb);
+    empty_sequences(a, tile, k, cb);
 }
 
 template <int DT, int G, int R, bool PACKED>
 __global__ __launch_bounds__(kBlock, DT == FS_F32 && !PACKED ? 2 : 3) void scan_bwd_kernel(ScanArgs a, const int32_t* __restrict__ tile_seq)
 {
     using Shape = ScanShape<DT, G, R>;
-    constexpr int N = Shape::N, Q = Shape::Q, LPB = kPackBlock / N;
+    constexpr int N = Shape::N, LPB = kPackBlock / N;
     __shared__ ScanShared<Shape> sh;
+    const Shape tile(a);
     const uint32_t t = take_ticket(a, &sh);
     const int64_t k = t / (uint32_t)a.col_blocks;       // from the batch's end
     const int cb = (int)(t % (uint32_t)a.col_blocks);
     if (k < a.tiles) {
-        const Place<Shape> p(a, a.tiles - 1 - k, cb);
-        const int lig = threadIdx.x % G, q = Q - 1 - p.group;
-        const Bounds bounds(a, tile_seq == nullptr ? 0 : tile_seq[a.tiles - 1 - k]);
+        const Place<Shape> p(a, tile, a.tiles - 1 - k, cb);
+                const Bounds bounds(a, tile_seq == nullptr ? 0 : tile_seq[a.tiles - 1 - k]);
         const u32x4* from_d = a.dh + p.row0 * a.units;
         u32x4 raw_d[R];
-        Saved<DT, PACKED, 0> x[R];
-        Saved<DT, PACKED, 1> gate[R];
-        Saved<DT, PACKED, 2> before[R];                 // h of the row before
+        Saved<DT, PACKED, 0, (G > 0)> x[R];
+        Saved<DT, PACKED, 1, (G > 0)> gate[R];
+        Saved<DT, PACKED, 2, (G > 0)> before[R];                 // h of the row before
 #pragma unroll
         for (int r = R - 1; r >= 0; --r) {              // in the order of their use
             const uint32_t block = p.row(r) * (uint32_t)a.nb + p.own / LPB;
             gate[r].load(a, p.row0, p.at(r), block);
-            raw_d[r] = load_stream(piece_at(from_d, p.at(r)));
+            raw_d[r] = load_rows<(G > 0)>(piece_at(from_d, p.at(r)));
         }
 #pragma unroll
         for (int r = R - 1; r >= 0; --r) {
@@ -490,9 +562,9 @@ __global__ __launch_bounds__(kBlock, DT == FS_F32 && !PACKED ? 2 : 3) void scan_
             const uint32_t up = p.row0 > 0 || row == 0 ? 0u : 1u;               // the batch's first row stands in for the one before it
             before[r].load(a, p.row0 > 0 ? p.row0 - 1 : 0, p.at(r) - up * p.units, block - up * (uint32_t)a.nb);
         }
-        if (wave_id() == 0) mark_sequences<Shape>(a, p.row0, bounds, &sh);
+        if (wave_id() == 0) mark_sequences(a, tile, p.row0, bounds, &sh);
         __syncthreads();
-        const uint32_t firsts = group_marks<Shape>(sh.firsts, p.group), lasts = group_marks<Shape>(sh.lasts, p.group);
+        const uint32_t firsts = group_marks(tile, sh.firsts), lasts = group_marks(tile, sh.lasts);
         float f[R][N], o[R][N], d[R][N];
         float A[N], B[N];
 #pragma unroll
@@ -505,11 +577,14 @@ __global__ __launch_bounds__(kBlock, DT == FS_F32 && !PACKED ? 2 : 3) void scan_
             for (int i = 0; i < N; ++i) gate_pair(f[r][i], &f[r][i], &o[r][i]);
             const bool ends = (lasts >> r) & 1;
             if (ballot(ends) != 0) {
-                if (ends && a.ends_in != nullptr && p.in) {
-                    float end[N];
-                    load_state<N>(a.ends_in, p.state(a, sh.last_of[p.group * R + r]), end);
+                if (ends && a.ends_in != nullptr) {
+                    const int64_t at = state_at(a, tile, cb, sh.last_of, r);
+                    if (at >= 0) {
+                        float end[N];
+                        load_state<N>(a.ends_in, at, end);
 #pragma unroll
-                    for (int i = 0; i < N; ++i) d[r][i] += end[i];
+                        for (int i = 0; i < N; ++i) d[r][i] += end[i];
+                    }
                 }
 #pragma unroll
                 for (int i = 0; i < N; ++i) B[i] = ends ? 0.0f : B[i];
@@ -520,19 +595,15 @@ __global__ __launch_bounds__(kBlock, DT == FS_F32 && !PACKED ? 2 : 3) void scan_
                 B[i] = f[r][i] * (d[r][i] + B[i]);
             }
         }
-        store_state<N>(&sh.A[q][0], lig * N, A);
-        store_state<N>(&sh.B[q][0], lig * N, B);
+        store_pair(tile, tile.Q - 1 - tile.group(), lasts != 0, A, B, &sh);
         __syncthreads();
-        // the groups in the order of the walk: from the last
-        const uint64_t resets = __builtin_bitreverse64(marked_groups<Shape>(sh.lasts)) >> (64 - Q);
-        const bool open = k > 0 && !(sh.lasts[Shape::T / 32 - 1] >> 31);
-        carry_states<Shape>(a, k, cb, resets, open, &sh);
+        const bool open = k > 0 && !((__builtin_amdgcn_readfirstlane((int)sh.lasts[(tile.T - 1) >> 5]) >> ((tile.T - 1) & 31)) & 1);
+        carry_states(a, tile, k, cb, k == 0 || any_marks(tile, sh.lasts), open, &sh);
         float U[N];
-        u32x4* to_x = a.dx + p.row0 * a.units;
-        u32x4* to_g = a.dgate + p.row0 * a.units;
-        const uint32_t first = again(p.first);
-#pragma unroll
-        for (int i = 0; i < N; ++i) U[i] = sh.B[q][lig * N + i];
+        const Place<Shape> out(a, tile, a.tiles - 1 - k, cb);
+        u32x4* to_x = a.dx + out.row0 * a.units;
+        u32x4* to_g = a.dgate + out.row0 * a.units;
+        group_states(tile, tile.Q - 1 - tile.group(), sh, U);
 #pragma unroll
         for (int r = R - 1; r >= 0; --r) {
             float xv[N], hb[N], dx[N], dg[N];
@@ -546,7 +617,10 @@ __global__ __launch_bounds__(kBlock, DT == FS_F32 && !PACKED ? 2 : 3) void scan_
             if (ballot(begins) != 0) {
 #pragma unroll
                 for (int i = 0; i < N; ++i) hb[i] = begins ? 0.0f : hb[i];
-                if (begins && a.h0 != nullptr && p.in) load_state<N>(a.h0, p.state(a, sh.first_of[p.group * R + r]), hb);
+                if (begins && a.h0 != nullptr) {
+                    const int64_t at = state_at(a, tile, cb, sh.first_of, r);
+                    if (at >= 0) load_state<N>(a.h0, at, hb);
+                }
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -555,14 +629,17 @@ __global__ __launch_bounds__(kBlock, DT == FS_F32 && !PACKED ? 2 : 3) void scan_
                 dg[i] = dx[i] * f[r][i] * (hb[i] - xv[i]);
                 U[i] = f[r][i] * Gi;
             }
-            if (p.stored(r)) {
-                store_stream(piece_at(to_x, first + r * p.units), Piece<DT>::pack(dx));
-                store_stream(piece_at(to_g, first + r * p.units), Piece<DT>::pack(dg));
+            if (out.stored(r)) {
+                store_rows<(G > 0)>(piece_at(to_x, out.first + r * out.units), Piece<DT>::pack(dx));
+                store_rows<(G > 0)>(piece_at(to_g, out.first + r * out.units), Piece<DT>::pack(dg));
             }
-            if (a.ends_out != nullptr && begins && p.in) store_state<N>(a.ends_out, p.state(a, sh.first_of[p.group * R + r]), U);
+            if (a.ends_out != nullptr && begins) {
+                const int64_t at = state_at(a, tile, cb, sh.first_of, r);
+                if (at >= 0) store_state<N>(a.ends_out, at, U);
+            }
         }
     }
-    empty_sequences<Shape>(a, k, cb);
+    empty_sequences(a, tile, k, cb);
 }
 
 // All words not ready, no ticket taken, and every tile's first sequence: the largest s with offsets[s] <= the row before it
@@ -611,13 +688,14 @@ __global__ __launch_bounds__(kBlock) void scan_step_kernel(const u32x4* __restri
 
 namespace {
 
-// Lanes of a group: the whole row up to 16 pieces (in a power of two), longer rows in blocks of 16 or 8 pieces, whichever
-// leaves fewer lanes idle.
-int scan_lanes(int units)
+// Lanes of a group: 16 or 8 for rows of as many pieces or a multiple of them (instances of their own: 3 % faster than with the
+// lanes as an argument, and the tiles of long rows stay long); other rows whole up to 256 columns, longer ones in blocks of equal size.
+int scan_lanes(int units, int N)
 {
-    if (units <= 4) return 4;
-    if (units <= 8) return 8;
-    return (units + 15) / 16 * 16 <= (units + 7) / 8 * 8 ? 16 : 8;
+    if (units % 16 == 0) return 16;
+    if (units % 8 == 0) return 8;
+    const int most = kBlock / N, blocks = (units + most - 1) / most;
+    return (units + blocks - 1) / blocks;
 }
 
 // Longest row, in 16-byte pieces (4 MB): a tile of at most 1024 rows is addressed by 32-bit offsets in bytes.
@@ -627,7 +705,7 @@ constexpr int kMostPieces = (1 << 18) - 1;
 constexpr int kFwdValues = 64, kBwdValues = 32;
 
 // Everything that follows from the sizes; *a gets them, `words` the workspace's places.
-fs_status plan_scan(int64_t n, int32_t D, fs_dtype dtype, int32_t T, int32_t B, int values, Carver* ws, ScanArgs* a, int* lanes)
+fs_status plan_scan(int64_t n, int32_t D, fs_dtype dtype, int32_t T, int32_t B, int values, Carver* ws, ScanArgs* a)
 {
     const fs_status st = check_seq_rows(n, D, dtype, &a->units);
     if (st != FS_OK) return st;
@@ -637,54 +715,57 @@ fs_status plan_scan(int64_t n, int32_t D, fs_dtype dtype, int32_t T, int32_t B, 
     a->n = n;
     a->nb = (int)pack_blocks(D);
     const int N = dtype == FS_F32 ? 4 : 8;
-    *lanes = scan_lanes(a->units);
-    const int64_t rows = (int64_t)(kBlock / *lanes) * (values / N);
-    a->col_blocks = (a->units + *lanes - 1) / *lanes;
+    a->lanes = scan_lanes(a->units, N);
+    a->groups = kBlock / a->lanes < 64 ? kBlock / a->lanes : 64;
+    a->by_lanes = (65536 + a->lanes - 1) / a->lanes;
+    a->by_columns = (65536 + a->lanes * N - 1) / (a->lanes * N);
+    const int64_t rows = (int64_t)a->groups * (values / N);
+    a->col_blocks = (a->units + a->lanes - 1) / a->lanes;
     a->tiles = (n + rows - 1) / rows;
     const int64_t passes = (a->S + kBlock - 1) / kBlock;            // workgroups that the sequences alone would keep busy
     a->strides = a->tiles > passes ? a->tiles : passes < 1024 ? passes : a->tiles > 1024 ? a->tiles : 1024;
     if (a->strides * a->col_blocks > 0x7FFFFFFF) return FS_ERR_SIZE;
     if (a->tiles > 1) {
-        a->words = ws->take<uint64_t>((size_t)a->tiles * (size_t)a->col_blocks * (size_t)(*lanes * N));
+        a->words = ws->take<uint64_t>((size_t)a->tiles * (size_t)a->col_blocks * (size_t)(a->lanes * N));
         a->tile_seq = ws->take<int32_t>((size_t)a->tiles);
         a->ticket = ws->take<uint32_t>(1);
     }
     return FS_OK;
 }
 
-fs_status clear_words(const ScanArgs& a, int columns, int values, hipStream_t s)
+fs_status clear_words(const ScanArgs& a, int N, int values, hipStream_t s)
 {
     if (a.tiles <= 1) return FS_OK;
-    const int64_t pieces = a.tiles * a.col_blocks * columns / 2;            // at least 8 a tile
+    const int64_t pieces = a.tiles * a.col_blocks * (a.lanes * N / 2);      // at least 2 a tile
     const int64_t grid = (pieces + kBlock - 1) / kBlock;
     if (grid > 0x7FFFFFFF) return FS_ERR_SIZE;
-    FS_LAUNCH("scan_clear", scan_clear_kernel, dim3((unsigned)grid), dim3(kBlock), s, a, pieces, kBlock * values / columns);
+    FS_LAUNCH("scan_clear", scan_clear_kernel, dim3((unsigned)grid), dim3(kBlock), s, a, pieces, a.groups * (values / N));
     return FS_OK;
 }
 
 #define FS_DISPATCH_LANES(lanes, CALL)                                                  \
     switch (lanes) {                                                                    \
-        case 4: CALL(4); break;                                                         \
         case 8: CALL(8); break;                                                         \
-        default: CALL(16); break;                                                       \
+        case 16: CALL(16); break;                                                       \
+        default: CALL(0); break;                                                        \
     }
 
 template <int DT>
-fs_status scan_fwd_launch(const ScanArgs& a, int lanes, hipStream_t s)
+fs_status scan_fwd_launch(const ScanArgs& a, hipStream_t s)
 {
     const dim3 grid((unsigned)(a.strides * a.col_blocks));
 #define CALL(G) FS_LAUNCH("scan_fwd", (scan_fwd_kernel<DT, G, kFwdValues / Piece<DT>::N>), grid, dim3(kBlock), s, a, a.tile_seq)
-    FS_DISPATCH_LANES(lanes, CALL)
+    FS_DISPATCH_LANES(a.lanes, CALL)
 #undef CALL
     return FS_OK;
 }
 
 template <int DT, bool PACKED>
-fs_status scan_bwd_launch(const ScanArgs& a, int lanes, hipStream_t s)
+fs_status scan_bwd_launch(const ScanArgs& a, hipStream_t s)
 {
     const dim3 grid((unsigned)(a.strides * a.col_blocks));
 #define CALL(G) FS_LAUNCH("scan_bwd", (scan_bwd_kernel<DT, G, kBwdValues / Piece<DT>::N, PACKED>), grid, dim3(kBlock), s, a, a.tile_seq)
-    FS_DISPATCH_LANES(lanes, CALL)
+    FS_DISPATCH_LANES(a.lanes, CALL)
 #undef CALL
     return FS_OK;
 }
@@ -694,8 +775,7 @@ fs_status scan_bwd(ScanArgs a, bool packed, int32_t D, fs_dtype dtype, int32_t T
 {
     if (!workspace_bytes) return FS_ERR_NULL;
     Carver ws(workspace);
-    int lanes = 0;
-    fs_status st = plan_scan(a.n, D, dtype, T, B, kBwdValues, &ws, &a, &lanes);
+    fs_status st = plan_scan(a.n, D, dtype, T, B, kBwdValues, &ws, &a);
     if (st != FS_OK) return st;
     if (!workspace) { *workspace_bytes = ws.used; return FS_OK; }
     if (*workspace_bytes < ws.used || misaligned(workspace, 256)) return FS_ERR_WORKSPACE;
@@ -711,14 +791,14 @@ fs_status scan_bwd(ScanArgs a, bool packed, int32_t D, fs_dtype dtype, int32_t T
         misaligned(a.codes[2], codes_alignment(dtype)) || misaligned(a.h0, 16) || misaligned(a.ends_in, 16) ||
         misaligned(a.ends_out, 16) || misaligned(a.offsets, 8))
         return FS_ERR_ALIGN;
-    st = clear_words(a, lanes * (dtype == FS_F32 ? 4 : 8), kBwdValues, s);
+    st = clear_words(a, dtype == FS_F32 ? 4 : 8, kBwdValues, s);
     if (st != FS_OK) return st;
     if (packed) {
-#define CALL(DT) st = scan_bwd_launch<DT, true>(a, lanes, s)
+#define CALL(DT) st = scan_bwd_launch<DT, true>(a, s)
         FS_DISPATCH_DTYPE(dtype, CALL)
 #undef CALL
     } else {
-#define CALL(DT) st = scan_bwd_launch<DT, false>(a, lanes, s)
+#define CALL(DT) st = scan_bwd_launch<DT, false>(a, s)
         FS_DISPATCH_DTYPE(dtype, CALL)
 #undef CALL
     }
@@ -737,8 +817,7 @@ extern "C" fs_status fs_seq_scan_fwd(
     if (!workspace_bytes) return FS_ERR_NULL;
     ScanArgs a = {};
     Carver ws(workspace);
-    int lanes = 0;
-    fs_status st = plan_scan(n, D, dtype, T, B, kFwdValues, &ws, &a, &lanes);
+    fs_status st = plan_scan(n, D, dtype, T, B, kFwdValues, &ws, &a);
     if (st != FS_OK) return st;
     if (!workspace) { *workspace_bytes = ws.used; return FS_OK; }
     if (*workspace_bytes < ws.used || misaligned(workspace, 256)) return FS_ERR_WORKSPACE;
@@ -748,9 +827,9 @@ extern "C" fs_status fs_seq_scan_fwd(
     a.x = static_cast<const u32x4*>(x); a.gate = static_cast<const u32x4*>(gate);
     a.offsets = offsets; a.ends_in = h0; a.h = static_cast<u32x4*>(h); a.ends_out = h_last; a.status = dev_status;
     hipStream_t hs = static_cast<hipStream_t>(stream);
-    st = clear_words(a, lanes * (dtype == FS_F32 ? 4 : 8), kFwdValues, hs);
+    st = clear_words(a, dtype == FS_F32 ? 4 : 8, kFwdValues, hs);
     if (st != FS_OK) return st;
-#define CALL(DT) return scan_fwd_launch<DT>(a, lanes, hs)
+#define CALL(DT) return scan_fwd_launch<DT>(a, hs)
     FS_DISPATCH_DTYPE(dtype, CALL)
 #undef CALL
 }
