@@ -519,31 +519,38 @@ def _like(fn: str, rows: torch.Tensor, same=(), float_rows=(), columns=(), per_r
     has to be the current one (the stream is).  The library takes sizes from the caller, so a tensor that is too small would
     be read past its end.  same: [n, D] in the type of rows; float_rows: [n, D] float32; columns: [D] float32;
     per_row: [n] float32; packed: pairs of codes [n, D] and exps [n, ceil(D / 32)]."""
-    if rows.dim() != 2:
-        raise ValueError(f"{fn}: rows are [n, D], got {tuple(rows.shape)}")
-    n, D = rows.shape
-    if rows.dtype not in _DTYPES:
-        raise TypeError(f"{fn}: rows are float32, float16 or bfloat16, got {rows.dtype}")
+    shape, kind = rows.shape, rows.dtype
+    if len(shape) != 2:
+        raise ValueError(f"{fn}: rows are [n, D], got {tuple(shape)}")
+    if kind not in _DTYPES:
+        raise TypeError(f"{fn}: rows are float32, float16 or bfloat16, got {kind}")
+    n, D = shape
     where = rows.get_device()
     if where >= 0 and where != _raw_device():
         raise ValueError(f"{fn}: tensors on device {where}, the current device is {_raw_device()}")
-
-    def need(t, shape, dtype):
-        if t is not None and (tuple(t.shape) != shape or t.dtype != dtype or t.get_device() != where):
-            raise ValueError(f"{fn}: expected {dtype} of shape {shape} on the device of the rows, got {t.dtype} {tuple(t.shape)} on {t.device}")
-
     for t in same:
-        need(t, (n, D), rows.dtype)
+        if t is not None and (t.shape != shape or t.dtype is not kind or t.get_device() != where):
+            raise _mismatch(fn, t, shape, kind)
+    f32 = torch.float32
     for t in float_rows:
-        need(t, (n, D), torch.float32)
+        if t is not None and (t.shape != shape or t.dtype is not f32 or t.get_device() != where):
+            raise _mismatch(fn, t, shape, f32)
     for t in columns:
-        need(t, (D,), torch.float32)
+        if t is not None and (t.shape != (D,) or t.dtype is not f32 or t.get_device() != where):
+            raise _mismatch(fn, t, (D,), f32)
     for t in per_row:
-        need(t, (n,), torch.float32)
+        if t is not None and (t.shape != (n,) or t.dtype is not f32 or t.get_device() != where):
+            raise _mismatch(fn, t, (n,), f32)
     for codes, exps in packed:
-        need(codes, (n, D), torch.int8)
-        need(exps, (n, (D + 31) // 32), torch.uint8)
-    return n, D, _DTYPES[rows.dtype]
+        if codes is not None and (codes.shape != shape or codes.dtype is not torch.int8 or codes.get_device() != where):
+            raise _mismatch(fn, codes, shape, torch.int8)
+        if exps is not None and (exps.shape != (n, (D + 31) // 32) or exps.dtype is not torch.uint8 or exps.get_device() != where):
+            raise _mismatch(fn, exps, (n, (D + 31) // 32), torch.uint8)
+    return n, D, _DTYPES[kind]
+
+
+def _mismatch(fn: str, t, shape, dtype) -> ValueError:
+    return ValueError(f"{fn}: expected {dtype} of shape {tuple(shape)} on the device of the rows, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 def fs_seq_pack8(x, codes, exps, raise_on_error: bool = True) -> int:

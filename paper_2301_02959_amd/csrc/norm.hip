@@ -3,8 +3,8 @@
 //   forward   m = mean(x), v = mean((x - m)^2), r = 1 / sqrt(v + eps), y = (x - m) r gamma + beta
 //   backward  u = (x - m) r, g = dy gamma:  dx = r (g - mean(g) - u mean(g u)), dgamma = sum over rows of dy u, dbeta = of dy
 //
-// HBM-bound: x read once and y written once; dy and x (or its checkpoint) read once and dx written once.  A row of up to 256
-// pieces of 16 bytes lies in the registers of a group of G lanes, P pieces a lane, so mean and squares are two passes over
+// HBM-bound: x read once and y written once; dy and x (or its checkpoint) read once and dx written once.  A row of up to
+// 1024 pieces of 16 bytes lies in the registers of G lanes, P pieces a lane, so mean and squares are two passes over
 // registers; longer rows are read three times by a workgroup each (kernels *_wide).  All sums are fp32.  The variance is taken
 // about the rounded mean and corrected by what that mean is off (s1 below), so a row of equal values far from zero
 // normalises to zeros.
@@ -34,6 +34,8 @@ struct NormArgs {
     uint8_t* exps;
     u32x4* dx;
     float* partial;                  // [workgroups][2][D]
+    float* dgamma;
+    float* dbeta;
 };
 
 template <int N>
@@ -69,11 +71,33 @@ __device__ __forceinline__ void write_codes(const NormArgs& a, int64_t row, int 
     if (piece % LPB == 0) a.exps[row * a.nb + piece / LPB] = (uint8_t)E;
 }
 
+// Sum over the workgroup, the same bits in every thread; `lds` holds kWavesPerBlock floats.
+__device__ __forceinline__ float block_sum(float v, float* lds)
+{
+    v = group_sum<kWave>(v);
+    __syncthreads();                       // lds may still be read from a previous call
+    if (lane_id() == 0) lds[wave_id()] = v;
+    __syncthreads();
+    float s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWavesPerBlock; ++w) s += lds[w];
+    return s;
+}
+
+// Sum over the G lanes of a row: a group of a wave, or the workgroup (whose threads all call it the same number of times).
+template <int G>
+__device__ __forceinline__ float row_sum(float v, float* lds)
+{
+    if constexpr (G <= kWave) return group_sum<G>(v);
+    else return block_sum(v, lds);
+}
+
 // A group of G lanes takes U rows, all their loads in flight at once.
 template <int DT, int G, int P, int U, bool PACK>
 __global__ __launch_bounds__(kBlock) void norm_fwd_kernel(NormArgs a)
 {
     constexpr int N = Piece<DT>::N, kGroups = kBlock / G;
+    __shared__ float lds[kWavesPerBlock];
     const int lig = threadIdx.x % G, group = threadIdx.x / G;
     const int64_t row0 = (int64_t)blockIdx.x * (kGroups * U) + group;
     u32x4 raw[U][P];
@@ -105,7 +129,7 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_kernel(NormArgs a)
             for (int i = 0; i < N; ++i) s += c[p][i];
             if constexpr (PACK) write_codes<DT, G>(a, row, lig + p * G, row < a.n && lig + p * G < a.units, c[p]);
         }
-        float mean = group_sum<G>(s) * a.inv_D;
+        float mean = row_sum<G>(s, lds) * a.inv_D;
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
@@ -117,8 +141,8 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_kernel(NormArgs a)
                 s2 = fmaf(c[p][i], c[p][i], s2);
             }
         }
-        const float off = group_sum<G>(s1) * a.inv_D;
-        const float var = fmaf(-off, off, group_sum<G>(s2) * a.inv_D);
+        const float off = row_sum<G>(s1, lds) * a.inv_D;
+        const float var = fmaf(-off, off, row_sum<G>(s2, lds) * a.inv_D);
         const float rstd = 1.0f / sqrtf(fmaxf(var, 0.0f) + a.eps);
         mean += off;
         if (row >= a.n) continue;
@@ -134,20 +158,7 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_kernel(NormArgs a)
     }
 }
 
-// Sum over the workgroup, the same bits in every thread; `lds` holds kWavesPerBlock floats.
-__device__ __forceinline__ float block_sum(float v, float* lds)
-{
-    v = group_sum<kWave>(v);
-    __syncthreads();                       // lds may still be read from a previous call
-    if (lane_id() == 0) lds[wave_id()] = v;
-    __syncthreads();
-    float s = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWavesPerBlock; ++w) s += lds[w];
-    return s;
-}
-
-// Rows of more than 256 pieces, one workgroup a row; the second and third pass read what the first has brought into the L2.
+// Rows of more than 1024 pieces, one workgroup a row; the second and third pass read what the first has brought into the L2.
 template <int DT, bool PACK>
 __global__ __launch_bounds__(kBlock) void norm_fwd_wide_kernel(NormArgs a)
 {
@@ -224,11 +235,18 @@ struct XPiece {
     }
 };
 
-template <int DT, int G, int P, int U, bool PACKED>
+// SMALL: few rows in one launch.  The first workgroup goes over all of them and writes dgamma and dbeta, the others write
+// their rows of dx; what both read comes from the L2 the second time.  Where dx is dy the first one does everything (the
+// others would write what it still has to read), in the same order.
+template <int DT, int G, int P, int U, bool PACKED, bool SMALL>
 __global__ __launch_bounds__(kBlock) void norm_bwd_kernel(NormArgs a)
 {
     constexpr int N = Piece<DT>::N, kGroups = kBlock / G;
     __shared__ float lds[kGroups][2][G * N];
+    __shared__ float sums[kWavesPerBlock];
+    const bool adds = !SMALL || blockIdx.x == 0, writes = !SMALL || blockIdx.x != 0 || gridDim.x == 1;
+    const int64_t first = SMALL && blockIdx.x > 0 ? blockIdx.x - 1 : blockIdx.x;
+    const int64_t step = SMALL && adds ? 1 : gridDim.x;
     const int lig = threadIdx.x % G, group = threadIdx.x / G;
     float gamma[P][N], dg[P][N], db[P][N];
 #pragma unroll
@@ -238,7 +256,7 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_kernel(NormArgs a)
 #pragma unroll
         for (int i = 0; i < N; ++i) dg[p][i] = db[p][i] = 0.0f;
     }
-    for (int64_t r0 = (int64_t)blockIdx.x * (kGroups * U); r0 < a.n; r0 += (int64_t)gridDim.x * (kGroups * U)) {
+    for (int64_t r0 = first * (kGroups * U); r0 < a.n; r0 += step * (kGroups * U)) {
         u32x4 dy_raw[U][P];
         XPiece<DT, PACKED> x_raw[U][P];
         float mean[U], rstd[U];
@@ -272,14 +290,17 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_kernel(NormArgs a)
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     w[p][i] = in ? (w[p][i] - mean[u]) * rstd[u] : 0.0f;
-                    dg[p][i] = fmaf(dy[i], w[p][i], dg[p][i]);
-                    db[p][i] += dy[i];
+                    if (adds) {
+                        dg[p][i] = fmaf(dy[i], w[p][i], dg[p][i]);
+                        db[p][i] += dy[i];
+                    }
                     g[p][i] = dy[i] * gamma[p][i];
                     s1 += g[p][i];
                     s2 = fmaf(g[p][i], w[p][i], s2);
                 }
             }
-            const float m1 = group_sum<G>(s1) * a.inv_D, m2 = group_sum<G>(s2) * a.inv_D;
+            if (!writes) continue;
+            const float m1 = row_sum<G>(s1, sums) * a.inv_D, m2 = row_sum<G>(s2, sums) * a.inv_D;
             if (row >= a.n) continue;
 #pragma unroll
             for (int p = 0; p < P; ++p) {
@@ -291,6 +312,7 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_kernel(NormArgs a)
             }
         }
     }
+    if (!adds) return;
     const int64_t D = (int64_t)a.units * N;
     float* to = a.partial + (int64_t)blockIdx.x * 2 * D;
 #pragma unroll
@@ -307,35 +329,46 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_kernel(NormArgs a)
             float s = 0.0f;
 #pragma unroll 4
             for (int k = 0; k < kGroups; ++k) s += lds[k][which][col];
-            if (p * G * N + col < D) to[which * D + p * G * N + col] = s;
+            if (p * G * N + col >= D) continue;
+            if constexpr (SMALL) (which == 0 ? a.dgamma : a.dbeta)[p * G * N + col] = s;
+            else to[which * D + p * G * N + col] = s;
         }
     }
 }
 
-// dgamma and dbeta as the sums of the `rows` partial rows of 2 D columns: wave w of a workgroup adds rows w, w + 16, ... for
-// its 64 columns, then the 16 sums are added in order.
-constexpr int kGradSumWaves = 16;
-__global__ __launch_bounds__(kGradSumWaves * kWave) void norm_grad_sum_kernel(const float* __restrict__ partial, int64_t rows,
-                                                                             int64_t D, float* __restrict__ dgamma,
-                                                                             float* __restrict__ dbeta)
+// dgamma and dbeta as the sums of the `rows` partial rows of 2 D columns: a workgroup has 32 columns, thread (i, c) adds rows
+// i, i + 32, ... of its column c, 16 of them in flight; then the 32 sums are added in order.
+constexpr int kSumCols = 32, kSumRows = 32;
+__global__ __launch_bounds__(kSumCols * kSumRows) void norm_grad_sum_kernel(const float* __restrict__ partial, int rows, int64_t D,
+                                                                           float* __restrict__ dgamma, float* __restrict__ dbeta)
 {
-    __shared__ float lds[kGradSumWaves][kWave];
-    const int64_t col = (int64_t)blockIdx.x * kWave + lane_id();
+    __shared__ float lds[kSumRows][kSumCols];
+    const int c = threadIdx.x % kSumCols, i = threadIdx.x / kSumCols;
+    const int64_t col = (int64_t)blockIdx.x * kSumCols + c;
     float s = 0.0f;
     if (col < 2 * D) {
-#pragma unroll 8
-        for (int64_t r = wave_id(); r < rows; r += kGradSumWaves) s += partial[r * 2 * D + col];
+        const float* from = partial + col;
+        for (int r0 = i; r0 < rows; r0 += kSumRows * 16) {
+            float v[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int r = r0 + j * kSumRows;
+                v[j] = from[(int64_t)(r < rows ? r : i) * 2 * D];
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) s += r0 + j * kSumRows < rows ? v[j] : 0.0f;
+        }
     }
-    lds[wave_id()][lane_id()] = s;
+    lds[i][c] = s;
     __syncthreads();
-    if (wave_id() != 0 || col >= 2 * D) return;
+    if (i != 0 || col >= 2 * D) return;
     s = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kGradSumWaves; ++w) s += lds[w][lane_id()];
+    for (int j = 0; j < kSumRows; ++j) s += lds[j][c];
     if (col < D) dgamma[col] = s; else dbeta[col - D] = s;
 }
 
-// Rows of more than 256 pieces: dx by a workgroup a row.
+// Rows of more than 1024 pieces: dx by a workgroup a row.
 template <int DT, bool PACKED>
 __global__ __launch_bounds__(kBlock) void norm_bwd_wide_kernel(NormArgs a)
 {
@@ -406,43 +439,45 @@ __global__ __launch_bounds__(kBlock) void norm_cols_wide_kernel(NormArgs a)
 
 namespace {
 
-constexpr int kWidePieces = 256;             // longest row that lies in the registers of a wave: 4 pieces a lane
-constexpr int kBwdBlocks = 1024;             // workgroups (= partial rows) of a large backward pass
+constexpr int kWidePieces = 4 * kBlock;      // longest row that lies in the registers of a workgroup: 4 pieces a thread
+constexpr int kBwdBlocks = 512;              // workgroups (= partial rows) of a large backward pass
 constexpr int kWideChunks = 64;              // row chunks of the wide columns' sums
+constexpr int kSmallRounds = 8;              // rounds of one workgroup over all rows that are worth a launch less
 
-// Lanes (G) and pieces a lane (P) of a row.
-int lanes_of(int units)
-{
-    int G = 4;
-    while (G < units && G < kWave) G *= 2;
-    return G;
-}
-
-// G, P of a row as constants: CALL(G, P)
+// Lanes (G) and pieces a lane (P) of a row as constants: CALL(G, P).  Up to 256 pieces a wave or a part of it has the row, up
+// to 1024 the workgroup.
 #define FS_DISPATCH_ROW(units, CALL)                                                    \
     do {                                                                                \
-        if ((units) > 128) { CALL(64, 4); }                                             \
+        if ((units) > 512) { CALL(256, 4); }                                            \
+        else if ((units) > 256) { CALL(256, 2); }                                       \
+        else if ((units) > 128) { CALL(64, 4); }                                        \
         else if ((units) > 64) { CALL(64, 2); }                                         \
-        else switch (lanes_of(units)) {                                                 \
-            case 4: CALL(4, 1); break;                                                  \
-            case 8: CALL(8, 1); break;                                                  \
-            case 16: CALL(16, 1); break;                                                \
-            case 32: CALL(32, 1); break;                                                \
-            default: CALL(64, 1); break;                                                \
-        }                                                                               \
+        else if ((units) > 32) { CALL(64, 1); }                                         \
+        else if ((units) > 16) { CALL(32, 1); }                                         \
+        else if ((units) > 8) { CALL(16, 1); }                                          \
+        else if ((units) > 4) { CALL(8, 1); }                                           \
+        else { CALL(4, 1); }                                                            \
     } while (0)
 
-constexpr int fwd_rows(int P) { return P == 1 ? 4 : P == 2 ? 2 : 1; }
-constexpr int bwd_rows(int P) { return P == 1 ? 2 : 1; }
+constexpr int fwd_rows(int P) { return P == 4 ? 1 : 2; }
+constexpr int bwd_rows(int P) { return P == 1 ? 4 : 1; }
+
+// Rows of a workgroup's round in the backward pass.
+int64_t bwd_round(int units)
+{
+#define CALL(G, P) return (int64_t)(kBlock / G) * bwd_rows(P)
+    FS_DISPATCH_ROW(units, CALL);
+#undef CALL
+}
 
 int64_t bwd_blocks(int64_t n, int units)
 {
     if (units > kWidePieces) return n < kWideChunks ? n : kWideChunks;
-    const int P = units > 128 ? 4 : units > 64 ? 2 : 1;
-    const int64_t per = (int64_t)(kBlock / lanes_of(units)) * bwd_rows(P);
-    const int64_t need = (n + per - 1) / per;
+    const int64_t per = bwd_round(units), need = (n + per - 1) / per;
     return need < kBwdBlocks ? need : kBwdBlocks;
 }
+
+bool bwd_small(int64_t n, int units) { return units <= kWidePieces && n <= kSmallRounds * bwd_round(units); }
 
 template <int DT>
 fs_status norm_fwd_launch(const NormArgs& a, hipStream_t s)
@@ -475,7 +510,12 @@ fs_status norm_bwd_launch(const NormArgs& a, hipStream_t s)
                   dim3(kBlock), s, a);
         return FS_OK;
     }
-#define CALL(G, P) FS_LAUNCH("norm_bwd", (norm_bwd_kernel<DT, G, P, bwd_rows(P), PACKED>), dim3(blocks), dim3(kBlock), s, a)
+#define CALL(G, P)                                                                                                        \
+    do {                                                                                                                  \
+        constexpr int U = bwd_rows(P);                                                                                    \
+        if (bwd_small(a.n, a.units)) FS_LAUNCH("norm_bwd", (norm_bwd_kernel<DT, G, P, U, PACKED, true>), dim3(a.dx == a.dy ? 1 : blocks + 1), dim3(kBlock), s, a); \
+        else FS_LAUNCH("norm_bwd", (norm_bwd_kernel<DT, G, P, U, PACKED, false>), dim3(blocks), dim3(kBlock), s, a);      \
+    } while (0)
     FS_DISPATCH_ROW(a.units, CALL);
 #undef CALL
     return FS_OK;
@@ -499,6 +539,8 @@ fs_status norm_bwd(NormArgs a, bool packed, int32_t D, fs_dtype dtype, float* dg
         return FS_ERR_ALIGN;
     a.nb = (int)pack_blocks(D);
     a.inv_D = 1.0f / (float)D;
+    a.dgamma = dgamma;
+    a.dbeta = dbeta;
     if (a.n > 0) {
         fs_status rc = FS_OK;
         if (packed) {
@@ -510,10 +552,10 @@ fs_status norm_bwd(NormArgs a, bool packed, int32_t D, fs_dtype dtype, float* dg
             FS_DISPATCH_DTYPE(dtype, CALL)
 #undef CALL
         }
-        if (rc != FS_OK) return rc;
+        if (rc != FS_OK || bwd_small(a.n, a.units)) return rc;
     }
-    FS_LAUNCH("norm_grad_sum", norm_grad_sum_kernel, dim3((unsigned)((2 * (int64_t)D + kWave - 1) / kWave)),
-              dim3(kGradSumWaves * kWave), s, a.partial, blocks, (int64_t)D, dgamma, dbeta);
+    FS_LAUNCH("norm_grad_sum", norm_grad_sum_kernel, dim3((unsigned)((2 * (int64_t)D + kSumCols - 1) / kSumCols)),
+              dim3(kSumCols * kSumRows), s, a.partial, (int)blocks, (int64_t)D, dgamma, dbeta);
     return FS_OK;
 }
 
