@@ -53,9 +53,9 @@ __global__ __launch_bounds__(kBlock) void pack8_kernel(const u32x4* __restrict__
     uint32_t* to = codes + (p.row * units + p.piece) * (N / 4);
     if constexpr (N == 8) {
         const u32x2 c = {pack_four(v, E), pack_four(v + 4, E)};
-        *reinterpret_cast<u32x2*>(to) = c;
+        __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(to));
     } else {
-        *to = pack_four(v, E);
+        *to = pack_four(v, E);                          // (4 bytes a lane: streamed 229 us, 2 M rows of 128, through the caches 213)
     }
     if (threadIdx.x % LPB == 0) exps[p.row * nb + p.block] = (uint8_t)E;
 }
