@@ -633,14 +633,16 @@ fs_status fs_seq_norm_bwd_packed(
  *   h[n, D] in `dtype`; the recurrence itself runs on unrounded float32 states.
  *   h0[T*B, D], h_last[T*B, D] float32; h_last (may be NULL) = the state after
  *   the last row, of an empty sequence its h0 (or 0).  A gate of -infinity
- *   shuts out the state before it, one of +infinity keeps it.  h may be x.
+ *   shuts out the state before it, one of +infinity keeps it.  h may be x,
+ *   h_last may be h0.
  * fs_seq_scan_bwd -- gradients for dh[n, D] (of h) and dh_last (of h_last, may
  *   be NULL = 0), backwards along every sequence:
  *   G_t = dh_t + f_(t+1) G_(t+1)  (the last row: dh_t + dh_last[s]),
  *   dx_t = (1 - f_t) G_t,  dgate_t = G_t (h_(t-1) - x_t) f_t (1 - f_t),
  *   dh0[s] = f_first G_first (an empty sequence: dh_last[s] or 0; dh0 may be NULL).
  *   x, gate, h as the forward pass had and wrote them (h_(t-1) is read in
- *   `dtype`, h0 of the first row in float32).  dx or dgate may be dh.
+ *   `dtype`, h0 of the first row in float32).  dx or dgate may be dh, dh0 may
+ *   be dh_last.
  * fs_seq_scan_bwd_packed -- the same with x, gate and h given as checkpoints of
  *   fs_seq_pack8: 3 bytes a value and column held for the backward pass
  *   instead of 6 or 12.
@@ -652,9 +654,15 @@ fs_status fs_seq_norm_bwd_packed(
  * are neither read nor written.
  * Data faults: bad offsets (FS_DEV_BAD_OFFSETS) leave the outputs unspecified
  * but written in bounds.
+ * The same bits on every run, from one workspace or another: the recurrence
+ * is put together from stretches of rows that n and D alone decide.
+ * Workspace (not for the step): 8 bytes a column for every stretch of rows
+ * that a workgroup has at a time, less than 4 % of x forward and 7 % backward;
+ * nothing in it has to survive from call to call or start at any value.
  * Host faults: unknown dtype; n < 0, n >= 2^31, D < 1, T < 1, B < 1,
- * T*B >= 2^31 (FS_ERR_SIZE); NULL; alignment as above, h0, h_last, dh_last,
- * dh0 and the states 16-byte aligned too; workspace as everywhere.
+ * T*B >= 2^31, a row of 4 MB or more, over 64 GB in x (FS_ERR_SIZE); NULL;
+ * alignment as above, h0, h_last, dh_last, dh0 and the states 16-byte aligned
+ * too; workspace as everywhere.
  */
 fs_status fs_seq_scan_fwd(
     const void* x, const void* gate, int64_t n, int32_t D, fs_dtype dtype,

@@ -479,9 +479,37 @@ int64_t bwd_blocks(int64_t n, int units)
 
 bool bwd_small(int64_t n, int units) { return units <= kWidePieces && n <= kSmallRounds * bwd_round(units); }
 
+// The arguments from row r0 on, for `rows` rows.
+template <int DT>
+NormArgs part_of(NormArgs a, int64_t r0, int64_t rows)
+{
+    constexpr int N = Piece<DT>::N;
+    const auto skip = [&](auto*& p, int64_t n) { if (p != nullptr) p += n; };
+    skip(a.x, r0 * a.units); skip(a.dy, r0 * a.units); skip(a.y, r0 * a.units); skip(a.dx, r0 * a.units);
+    skip(a.x_codes, r0 * a.units * (N / 4)); skip(a.codes, r0 * a.units * (N / 4));
+    skip(a.x_exps, r0 * a.nb); skip(a.exps, r0 * a.nb);
+    skip(a.mean, r0); skip(a.rstd, r0);
+    a.n = rows;
+    return a;
+}
+
+// Rows of a forward launch.
+int64_t fwd_launch_rows(int units)
+{
+    if (units > kWidePieces) return kMostGrid;
+#define CALL(G, P) return kMostGrid * ((kBlock / G) * fwd_rows(P))
+    FS_DISPATCH_ROW(units, CALL);
+#undef CALL
+}
+
 template <int DT>
 fs_status norm_fwd_launch(const NormArgs& a, hipStream_t s)
 {
+    const int64_t most = fwd_launch_rows(a.units);
+    if (a.n > most) {
+        const fs_status rc = norm_fwd_launch<DT>(part_of<DT>(a, 0, most), s);
+        return rc != FS_OK ? rc : norm_fwd_launch<DT>(part_of<DT>(a, most, a.n - most), s);
+    }
     const bool pack = a.codes != nullptr;
     if (a.units > kWidePieces) {
         if (pack) FS_LAUNCH("norm_fwd_wide", (norm_fwd_wide_kernel<DT, true>), dim3((unsigned)a.n), dim3(kBlock), s, a);
@@ -505,7 +533,10 @@ fs_status norm_bwd_launch(const NormArgs& a, hipStream_t s)
 {
     const unsigned blocks = (unsigned)bwd_blocks(a.n, a.units);
     if (a.units > kWidePieces) {
-        FS_LAUNCH("norm_bwd_wide", (norm_bwd_wide_kernel<DT, PACKED>), dim3((unsigned)a.n), dim3(kBlock), s, a);
+        for (int64_t r0 = 0; r0 < a.n; r0 += kMostGrid) {
+            const int64_t rows = a.n - r0 < kMostGrid ? a.n - r0 : kMostGrid;
+            FS_LAUNCH("norm_bwd_wide", (norm_bwd_wide_kernel<DT, PACKED>), dim3((unsigned)rows), dim3(kBlock), s, part_of<DT>(a, r0, rows));
+        }
         FS_LAUNCH("norm_cols_wide", (norm_cols_wide_kernel<DT, PACKED>), dim3((unsigned)((a.units + kBlock - 1) / kBlock), blocks),
                   dim3(kBlock), s, a);
         return FS_OK;

@@ -82,12 +82,13 @@ __global__ __launch_bounds__(kBlock) void unpack8_kernel(const uint32_t* __restr
 }
 
 namespace {
-// Grid of a launch over (row, block of columns): 0 = too large.
-unsigned pack_grid(int64_t n, int nb, int lpb)
+// Rows of one launch, and the grid for `rows` of them: (row, block of columns) by LPB lanes.
+int64_t pack_launch_rows(int nb, int lpb) { return kMostGrid * (kBlock / lpb) / nb; }
+
+dim3 pack_grid(int64_t rows, int nb, int lpb)
 {
     const int64_t per = kBlock / lpb;
-    const int64_t grid = (n * nb + per - 1) / per;              // n < 2^31 and nb <= 2^26: no overflow
-    return grid > 0x7FFFFFFF ? 0u : (unsigned)grid;
+    return dim3((unsigned)((rows * nb + per - 1) / per));
 }
 }  // namespace
 
@@ -103,12 +104,15 @@ extern "C" fs_status fs_seq_pack8(const void* x, int64_t n, int32_t D, fs_dtype 
     if (!x || !codes || !exps) return FS_ERR_NULL;
     if (misaligned(x, 16) || misaligned(codes, codes_alignment(dtype))) return FS_ERR_ALIGN;
     const int nb = (int)pack_blocks(D);
-    const unsigned grid = pack_grid(n, nb, dtype == FS_F32 ? 8 : 4);
-    if (grid == 0) return FS_ERR_SIZE;
-#define CALL(DT) FS_LAUNCH("pack8", pack8_kernel<DT>, dim3(grid), dim3(kBlock), static_cast<hipStream_t>(stream),        \
-                           static_cast<const u32x4*>(x), n, units, nb, reinterpret_cast<uint32_t*>(codes), exps)
-    FS_DISPATCH_DTYPE(dtype, CALL)
+    const int lpb = dtype == FS_F32 ? 8 : 4;
+    const int64_t most = pack_launch_rows(nb, lpb);
+    for (int64_t r0 = 0; r0 < n; r0 += most) {
+        const int64_t rows = n - r0 < most ? n - r0 : most;
+#define CALL(DT) FS_LAUNCH("pack8", pack8_kernel<DT>, pack_grid(rows, nb, lpb), dim3(kBlock), static_cast<hipStream_t>(stream),      \
+                           static_cast<const u32x4*>(x) + r0 * units, rows, units, nb, reinterpret_cast<uint32_t*>(codes + r0 * D), exps + r0 * nb)
+        FS_DISPATCH_DTYPE(dtype, CALL)
 #undef CALL
+    }
     return FS_OK;
 }
 
@@ -122,11 +126,14 @@ extern "C" fs_status fs_seq_unpack8(const int8_t* codes, const uint8_t* exps, in
     if (!x || !codes || !exps) return FS_ERR_NULL;
     if (misaligned(x, 16) || misaligned(codes, codes_alignment(dtype))) return FS_ERR_ALIGN;
     const int nb = (int)pack_blocks(D);
-    const unsigned grid = pack_grid(n, nb, dtype == FS_F32 ? 8 : 4);
-    if (grid == 0) return FS_ERR_SIZE;
-#define CALL(DT) FS_LAUNCH("unpack8", unpack8_kernel<DT>, dim3(grid), dim3(kBlock), static_cast<hipStream_t>(stream),    \
-                           reinterpret_cast<const uint32_t*>(codes), exps, n, units, nb, static_cast<u32x4*>(x))
-    FS_DISPATCH_DTYPE(dtype, CALL)
+    const int lpb = dtype == FS_F32 ? 8 : 4;
+    const int64_t most = pack_launch_rows(nb, lpb);
+    for (int64_t r0 = 0; r0 < n; r0 += most) {
+        const int64_t rows = n - r0 < most ? n - r0 : most;
+#define CALL(DT) FS_LAUNCH("unpack8", unpack8_kernel<DT>, pack_grid(rows, nb, lpb), dim3(kBlock), static_cast<hipStream_t>(stream),  \
+                           reinterpret_cast<const uint32_t*>(codes + r0 * D), exps + r0 * nb, rows, units, nb, static_cast<u32x4*>(x) + r0 * units)
+        FS_DISPATCH_DTYPE(dtype, CALL)
 #undef CALL
+    }
     return FS_OK;
 }

@@ -724,7 +724,7 @@ fs_status plan_scan(int64_t n, int32_t D, fs_dtype dtype, int32_t T, int32_t B, 
     a->tiles = (n + rows - 1) / rows;
     const int64_t passes = (a->S + kBlock - 1) / kBlock;            // workgroups that the sequences alone would keep busy
     a->strides = a->tiles > passes ? a->tiles : passes < 1024 ? passes : a->tiles > 1024 ? a->tiles : 1024;
-    if (a->strides * a->col_blocks > 0x7FFFFFFF) return FS_ERR_SIZE;
+    if (a->strides * a->col_blocks > kMostGrid) return FS_ERR_SIZE;         // (over 64 GB a tensor)
     if (a->tiles > 1) {
         a->words = ws->take<uint64_t>((size_t)a->tiles * (size_t)a->col_blocks * (size_t)(a->lanes * N));
         a->tile_seq = ws->take<int32_t>((size_t)a->tiles);
@@ -737,8 +737,7 @@ fs_status clear_words(const ScanArgs& a, int N, int values, hipStream_t s)
 {
     if (a.tiles <= 1) return FS_OK;
     const int64_t pieces = a.tiles * a.col_blocks * (a.lanes * N / 2);      // at least 2 a tile
-    const int64_t grid = (pieces + kBlock - 1) / kBlock;
-    if (grid > 0x7FFFFFFF) return FS_ERR_SIZE;
+    const int64_t grid = (pieces + kBlock - 1) / kBlock;                    // fewer than the tiles' workgroups, in plan_scan's bound
     FS_LAUNCH("scan_clear", scan_clear_kernel, dim3((unsigned)grid), dim3(kBlock), s, a, pieces, a.groups * (values / N));
     return FS_OK;
 }
@@ -879,7 +878,7 @@ extern "C" fs_status fs_seq_scan_step(
     if (misaligned(x, 16) || misaligned(gate, 16) || misaligned(state, 16) || misaligned(state_out, 16) || misaligned(h, 16))
         return FS_ERR_ALIGN;
     const int64_t pieces = m * units, grid = (pieces + kBlock - 1) / kBlock;
-    if (grid > 0x7FFFFFFF) return FS_ERR_SIZE;
+    if (grid > kMostGrid) return FS_ERR_SIZE;                               // (64 GB a tensor)
 #define CALL(DT) FS_LAUNCH("scan_step", scan_step_kernel<DT>, dim3((unsigned)grid), dim3(kBlock), static_cast<hipStream_t>(stream),  \
                            static_cast<const u32x4*>(x), static_cast<const u32x4*>(gate), state, state_out, static_cast<u32x4*>(h), pieces)
     FS_DISPATCH_DTYPE(dtype, CALL)

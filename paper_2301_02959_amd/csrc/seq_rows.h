@@ -53,6 +53,9 @@ __device__ __forceinline__ float group_sum(float v)
     return v;
 }
 
+// A launch has fewer than 2^32 threads: the most workgroups of kBlock.  Longer batches go in several launches of whole rows.
+constexpr int64_t kMostGrid = (1LL << 32) / kBlock - 1;
+
 inline bool misaligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
 
 // Sizes and type of n rows of D elements; *units = 16-byte pieces of a row.

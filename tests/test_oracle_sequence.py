@@ -139,3 +139,32 @@ def test_recurrence_and_its_gradient():
         down[t, d] -= 1e-5
         # central difference: off by step^2 / 6 times a third derivative below 1 here, and by 1e-16 / 1e-5
         assert abs((loss(up) - loss(down)) / 2e-5 - dg[t, d]) < 1e-8
+
+
+def test_the_chains_gradient_against_differences():
+    """Rows -> norm -> recurrence (gates from the same normalised rows) -> a weighted sum, all in 64 bits: the gradients handed
+    back stage by stage against central differences of the whole."""
+    rng = np.random.default_rng(9)
+    offsets, D = [0, 4, 4, 5, 11], 6
+    x, dh = rng.standard_normal((11, D)), rng.standard_normal((11, D))
+    gamma, beta, scale = rng.standard_normal(D), rng.standard_normal(D), rng.standard_normal(D)
+
+    def forward(x_, gamma_, beta_):
+        y, mean, rstd = seq.norm_fwd(x_, gamma_, beta_, 1e-3)
+        h, _, _, _ = seq.scan_fwd(y, y * scale, offsets)
+        return y, mean, rstd, h
+
+    y, mean, rstd, h = forward(x, gamma, beta)
+    dy, dgate, _, _, _, _ = seq.scan_bwd(dh, None, y, y * scale, h, offsets)
+    dx, dgamma, dbeta = seq.norm_bwd(dy + dgate * scale, x, mean, rstd, gamma)
+    step = 1e-5
+    for name, of, grad in (("x", x, dx), ("gamma", gamma, dgamma), ("beta", beta, dbeta)):
+        for at in [np.unravel_index(i, of.shape) for i in rng.choice(of.size, 6, replace=False)]:
+            sides = []
+            for d in (step, -step):
+                moved = {"x": x.copy(), "gamma": gamma.copy(), "beta": beta.copy()}
+                moved[name][at] += d
+                sides.append((forward(moved["x"], moved["gamma"], moved["beta"])[3] * dh).sum())
+            # a central difference: step^2 / 6 times a third derivative (the norm's: up to 1 / eps^(3/2) = 3e4 times a few, were a
+            # row's deviations all below sqrt(eps); here they are near 1, so tens), and 1e-15 / step of rounding
+            assert abs((sides[0] - sides[1]) / (2 * step) - grad[at]) < 1e-7 * max(1, abs(grad[at])), (name, at)
