@@ -657,7 +657,7 @@ fs_status fs_seq_norm_bwd_packed(
  * The same bits on every run, from one workspace or another: the recurrence
  * is put together from stretches of rows that n and D alone decide.
  * Workspace (not for the step): 8 bytes a column for every stretch of rows
- * that a workgroup has at a time, less than 4 % of x forward and 7 % backward;
+ * that a workgroup has at a time, less than 4 % of x forward and 8 % backward;
  * nothing in it has to survive from call to call or start at any value.
  * Host faults: unknown dtype; n < 0, n >= 2^31, D < 1, T < 1, B < 1,
  * T*B >= 2^31, a row of 4 MB or more, over 64 GB in x (FS_ERR_SIZE); NULL;
