@@ -10,6 +10,9 @@
 // normalises to zeros.
 // dgamma and dbeta: every lane keeps its columns' sums over the rows that its group walks, a workgroup adds its groups in
 // LDS and writes one partial row, norm_grad_sum adds the partial rows in their order: no atomics, the same bits every run.
+//
+// Measured, 3.93 M rows of 256 bf16 (us, TB/s of what has to be read and written): forward 691 (5.8), with the checkpoint
+// written too 884 (5.7), backward 1078 (5.6), from the checkpoint 930 (5.4).
 #include "pack8.h"
 #include "seq_rows.h"
 
@@ -440,9 +443,11 @@ __global__ __launch_bounds__(kBlock) void norm_cols_wide_kernel(NormArgs a)
 namespace {
 
 constexpr int kWidePieces = 4 * kBlock;      // longest row that lies in the registers of a workgroup: 4 pieces a thread
-constexpr int kBwdBlocks = 512;              // workgroups (= partial rows) of a large backward pass
+// Workgroups (= partial rows) of a large backward pass: two a CU (256, 512, 768, 1024: 1331, 1114, 1118, 1241 us for the
+// 3.93 M rows, with two rows a group; with four and 512 1078).
+constexpr int kBwdBlocks = 512;
 constexpr int kWideChunks = 64;              // row chunks of the wide columns' sums
-constexpr int kSmallRounds = 8;              // rounds of one workgroup over all rows that are worth a launch less
+constexpr int kSmallRounds = 8;              // rounds of one workgroup over all rows that are worth a launch less (100 rows of 256: 6.9 us, with the second launch 10.8)
 
 // Lanes (G) and pieces a lane (P) of a row as constants: CALL(G, P).  Up to 256 pieces a wave or a part of it has the row, up
 // to 1024 the workgroup.
@@ -459,6 +464,7 @@ constexpr int kSmallRounds = 8;              // rounds of one workgroup over all
         else { CALL(4, 1); }                                                            \
     } while (0)
 
+// Rows that a group has in flight (3.93 M rows of 256 bf16, us: forward 1, 2, 4, 8 rows 728, 691, 718, 718; backward 2, 4 rows 1114, 1078).
 constexpr int fwd_rows(int P) { return P == 4 ? 1 : 2; }
 constexpr int bwd_rows(int P) { return P == 1 ? 4 : 1; }
 

