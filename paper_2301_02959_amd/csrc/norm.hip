@@ -539,12 +539,13 @@ fs_status norm_bwd_launch(const NormArgs& a, hipStream_t s)
 {
     const unsigned blocks = (unsigned)bwd_blocks(a.n, a.units);
     if (a.units > kWidePieces) {
+        // the sums first: dx may be dy
+        FS_LAUNCH("norm_cols_wide", (norm_cols_wide_kernel<DT, PACKED>), dim3((unsigned)((a.units + kBlock - 1) / kBlock), blocks),
+                  dim3(kBlock), s, a);
         for (int64_t r0 = 0; r0 < a.n; r0 += kMostGrid) {
             const int64_t rows = a.n - r0 < kMostGrid ? a.n - r0 : kMostGrid;
             FS_LAUNCH("norm_bwd_wide", (norm_bwd_wide_kernel<DT, PACKED>), dim3((unsigned)rows), dim3(kBlock), s, part_of<DT>(a, r0, rows));
         }
-        FS_LAUNCH("norm_cols_wide", (norm_cols_wide_kernel<DT, PACKED>), dim3((unsigned)((a.units + kBlock - 1) / kBlock), blocks),
-                  dim3(kBlock), s, a);
         return FS_OK;
     }
 #define CALL(G, P)                                                                                                        \

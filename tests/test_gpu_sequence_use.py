@@ -302,3 +302,31 @@ def test_the_most_rows_a_call_admits():
     assert np.array_equal(host(y[n - tail:]), seq.unpack8(wc, we).astype(np.float16).astype(np.float64))
     del x, y, codes, exps
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("units", [1, 16, 65, 300, 1024, 1100])
+@pytest.mark.parametrize("n", [3, 600])
+def test_norm_gradients_in_place_at_every_width(units, n):
+    """dx may be dy whatever kernels the width takes: the sums over dy have to be done with it first."""
+    D = width(units, torch.bfloat16)
+    gen = generator(units + n)
+    x, dy = rows(gen, n, D, torch.bfloat16), rows(gen, n, D, torch.bfloat16)
+    gamma, beta = torch.randn(D, generator=gen).to(DEV), torch.zeros(D, device=DEV)
+    y, mean, rstd = torch.empty_like(x), torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    codes, exps = torch.empty(n, D, dtype=torch.int8, device=DEV), torch.empty(n, -(-D // 32), dtype=torch.uint8, device=DEV)
+    fs.fs_seq_norm_fwd(x, gamma, beta, EPS, y, mean, rstd, codes, exps)
+    for packed in (False, True):
+        got = []
+        for in_place in (False, True):
+            d = dy.clone()
+            dx = d if in_place else torch.empty_like(d)
+            dg, db = torch.empty(D, device=DEV), torch.empty(D, device=DEV)
+            if packed:
+                fs.fs_seq_norm_bwd_packed(d, codes, exps, mean, rstd, gamma, dx, dg, db)
+            else:
+                fs.fs_seq_norm_bwd(d, x, mean, rstd, gamma, dx, dg, db)
+            got.append((dx, dg, db))
+        assert equal(*got)
+    z = x.clone()
+    fs.fs_seq_norm_fwd(z, gamma, beta, EPS, z)
+    assert same_bits(z, y)
