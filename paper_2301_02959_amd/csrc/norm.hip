@@ -567,7 +567,7 @@ fs_status norm_bwd(NormArgs a, bool packed, int32_t D, fs_dtype dtype, float* dg
     if (st != FS_OK) return st;
     Carver ws(workspace);
     const int64_t blocks = bwd_blocks(a.n, a.units);
-    a.partial = ws.take<float>((size_t)blocks * 2 * (size_t)D);
+    a.partial = ws.take<float>((size_t)(blocks > 0 ? blocks : 1) * 2 * (size_t)D);      // never nothing: a null workspace is a question
     if (!workspace) { *workspace_bytes = ws.used; return FS_OK; }
     if (*workspace_bytes < ws.used || misaligned(workspace, 256)) return FS_ERR_WORKSPACE;
     if (!a.gamma || !dgamma || !dbeta) return FS_ERR_NULL;

@@ -807,10 +807,11 @@ fs_status plan_scan(int64_t n, int32_t D, fs_dtype dtype, int32_t T, int32_t B, 
     const int64_t passes = (a->S + kBlock - 1) / kBlock;            // workgroups that the sequences alone would keep busy
     a->strides = a->tiles > passes ? a->tiles : passes < 1024 ? passes : a->tiles > 1024 ? a->tiles : 1024;
     if (a->strides * a->col_blocks > kMostGrid) return FS_ERR_SIZE;         // (over 64 GB a tensor)
+    uint32_t* const ticket = ws->take<uint32_t>(1);                 // always: a workspace of no bytes could be null, which is a question
     if (a->tiles > 1) {
         a->words = ws->take<uint64_t>((size_t)(a->tiles + a->tiles / kSpan) * (size_t)a->col_blocks * (size_t)(a->lanes * N));
         a->tile_seq = ws->take<int32_t>((size_t)a->tiles);
-        a->ticket = ws->take<uint32_t>(1);
+        a->ticket = ticket;
     }
     return FS_OK;
 }

@@ -136,3 +136,12 @@ def test_the_binding_compares_shapes():
         fs.fs_seq_scan_step(x, x, z(4, 8, dtype=torch.float16), z(4, 8), x)
     with pytest.raises(TypeError):                       # all shapes fit, but this is host memory
         fs.fs_seq_scan_step(x, x, z(4, 8), z(4, 8), x)
+
+
+@pytest.mark.parametrize("name", sorted(k for k in BASE if "size" in BASE[k]))
+@pytest.mark.parametrize("n", [0, 1, 100])
+def test_a_workspace_is_never_of_no_bytes(name, n):
+    """A null workspace asks for the size, so a size of 0 would make a caller who allocates it ask again instead of running."""
+    asked = ctypes.c_size_t(0)
+    assert call(name, *dict(BASE[name], n=n, ws=None, size=ctypes.byref(asked)).values()) == 0
+    assert asked.value >= 4
