@@ -737,10 +737,11 @@ __global__ __launch_bounds__(kBlock) void scan_clear_kernel(ScanArgs a, int64_t 
     a.tile_seq[i] = (int32_t)lo;
 }
 
+// (No pointer is restricted: h may be x, state_out state.)
 // One token of every session: a 16-byte piece of x, gate and out to a lane, its states as fp32 beside it.
 template <int DT>
-__global__ __launch_bounds__(kBlock) void scan_step_kernel(const u32x4* __restrict__ x, const u32x4* __restrict__ gate,
-                                                           const float* state, float* state_out, u32x4* __restrict__ h, int64_t pieces)
+__global__ __launch_bounds__(kBlock) void scan_step_kernel(const u32x4* x, const u32x4* gate, const float* state,
+                                                           float* state_out, u32x4* h, int64_t pieces)
 {
     constexpr int N = Piece<DT>::N;
     const int64_t at = (int64_t)blockIdx.x * kBlock + threadIdx.x;

@@ -330,3 +330,15 @@ def test_norm_gradients_in_place_at_every_width(units, n):
     z = x.clone()
     fs.fs_seq_norm_fwd(z, gamma, beta, EPS, z)
     assert same_bits(z, y)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_step_in_place(dtype):
+    """h may be x and state_out may be state, both at once."""
+    m, D = 300, width(9, dtype)
+    gen = generator(3)
+    x, gate, state = rows(gen, m, D, dtype), rows(gen, m, D, dtype, 2.0, 1.5), torch.randn(m, D, generator=gen).to(DEV)
+    out, h = torch.empty_like(state), torch.empty_like(x)
+    fs.fs_seq_scan_step(x, gate, state, out, h)
+    fs.fs_seq_scan_step(x, gate, state, state, x)
+    assert same_bits(x, h) and same_bits(state, out)
