@@ -514,154 +514,122 @@ def fs_seq_grad_bwd_update(grad_out, sorted_rows, sorted_pos, m: int, R: int, we
     return _check("fs_seq_grad_bwd_update", call(_ptr(workspace), ctypes.byref(size)), raise_on_error)
 
 
-def _like(fn: str, rows: torch.Tensor, same=(), float_rows=(), columns=(), per_row=(), packed=()) -> Tuple[int, int, int]:
-    """(n, D, dtype) of `rows`, once the tensors that go with it are found to be of its sizes, its type and its device, which
-    has to be the current one (the stream is).  The library takes sizes from the caller, so a tensor that is too small would
-    be read past its end.  same: [n, D] in the type of rows; float_rows: [n, D] float32; columns: [D] float32;
-    per_row: [n] float32; packed: pairs of codes [n, D] and exps [n, ceil(D / 32)]."""
-    shape, kind = rows.shape, rows.dtype
-    if len(shape) != 2:
-        raise ValueError(f"{fn}: rows are [n, D], got {tuple(shape)}")
-    if kind not in _DTYPES:
-        raise TypeError(f"{fn}: rows are float32, float16 or bfloat16, got {kind}")
-    n, D = shape
+def _rows(fn: str, kinds: str, rows: torch.Tensor, *tensors, sequences: int = 0) -> tuple:
+    """(n, D, dtype, pointer of `rows`, pointers of the tensors that go with it ...), once those are found to be of its sizes and
+    on its device, which has to be the current one (the stream is).  The library takes sizes from the caller, so a tensor that is
+    too small would be read past its end.  A letter of `kinds` for each tensor, which may be None: s [n, D] of the type of rows;
+    f [n, D], c [D], r [n], t [sequences, D] float32; p [n, D] codes and e [n, ceil(D / 32)] exponents of a checkpoint;
+    o [sequences + 1] offsets."""
+    if _fit is not None and rows.is_cuda:
+        got = _fit(kinds, _raw_device(), sequences, rows, *tensors)
+        if got is not None:
+            return got
+    return _rows_checked(fn, kinds, rows, tensors, sequences)
+
+
+def _rows_checked(fn: str, kinds: str, rows: torch.Tensor, tensors: tuple, sequences: int) -> tuple:
+    if rows.dim() != 2:
+        raise ValueError(f"{fn}: rows are [n, D], got {tuple(rows.shape)}")
+    if rows.dtype not in _DTYPES:
+        raise TypeError(f"{fn}: rows are float32, float16 or bfloat16, got {rows.dtype}")
+    n, D = rows.shape
     where = rows.get_device()
     if where >= 0 and where != _raw_device():
         raise ValueError(f"{fn}: tensors on device {where}, the current device is {_raw_device()}")
-    for t in same:
-        if t is not None and (t.shape != shape or t.dtype is not kind or t.get_device() != where):
-            raise _mismatch(fn, t, shape, kind)
-    f32 = torch.float32
-    for t in float_rows:
-        if t is not None and (t.shape != shape or t.dtype is not f32 or t.get_device() != where):
-            raise _mismatch(fn, t, shape, f32)
-    for t in columns:
-        if t is not None and (t.shape != (D,) or t.dtype is not f32 or t.get_device() != where):
-            raise _mismatch(fn, t, (D,), f32)
-    for t in per_row:
-        if t is not None and (t.shape != (n,) or t.dtype is not f32 or t.get_device() != where):
-            raise _mismatch(fn, t, (n,), f32)
-    for codes, exps in packed:
-        if codes is not None and (codes.shape != shape or codes.dtype is not torch.int8 or codes.get_device() != where):
-            raise _mismatch(fn, codes, shape, torch.int8)
-        if exps is not None and (exps.shape != (n, (D + 31) // 32) or exps.dtype is not torch.uint8 or exps.get_device() != where):
-            raise _mismatch(fn, exps, (n, (D + 31) // 32), torch.uint8)
-    return n, D, _DTYPES[kind]
+    wanted = {"s": ((n, D), rows.dtype), "f": ((n, D), torch.float32), "c": ((D,), torch.float32), "r": ((n,), torch.float32),
+              "p": ((n, D), torch.int8), "e": ((n, (D + 31) // 32), torch.uint8), "o": ((sequences + 1,), torch.int64),
+              "t": ((sequences, D), torch.float32)}
+    for kind, t in zip(kinds, tensors):
+        shape, dtype = wanted[kind]
+        if t is not None and (tuple(t.shape) != shape or t.dtype != dtype or t.get_device() != where):
+            raise ValueError(f"{fn}: expected {dtype} of shape {shape} on the device of the rows, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return (n, D, _DTYPES[rows.dtype], _ptr(rows), *[_ptr(t) for t in tensors])
 
 
-def _mismatch(fn: str, t, shape, dtype) -> ValueError:
-    return ValueError(f"{fn}: expected {dtype} of shape {tuple(shape)} on the device of the rows, got {t.dtype} {tuple(t.shape)} on {t.device}")
+def _native_fit():
+    """_rows in native code, for plain tensors that fit; None where the native helper is not in use."""
+    if _ptr is _ptr_checked:
+        return None
+    from . import _marshal
+    return getattr(_marshal, "rows_that_fit", None)
+
+
+_fit = _native_fit()
 
 
 def fs_seq_pack8(x, codes, exps, raise_on_error: bool = True) -> int:
-    n, D, dtype = _like("fs_seq_pack8", x, packed=((codes, exps),))
-    code = _typed().fs_seq_pack8(_ptr(x, _ROWS), n, D, dtype, _ptr(codes, _I8), _ptr(exps, _U8), _stream())
-    return _check("fs_seq_pack8", code, raise_on_error)
+    n, D, dtype, x_, codes_, exps_ = _rows("fs_seq_pack8", "pe", x, codes, exps)
+    return _check("fs_seq_pack8", _typed().fs_seq_pack8(x_, n, D, dtype, codes_, exps_, _stream()), raise_on_error)
 
 
 def fs_seq_unpack8(codes, exps, x, raise_on_error: bool = True) -> int:
-    n, D, dtype = _like("fs_seq_unpack8", x, packed=((codes, exps),))
-    code = _typed().fs_seq_unpack8(_ptr(codes, _I8), _ptr(exps, _U8), n, D, dtype, _ptr(x, _ROWS), _stream())
-    return _check("fs_seq_unpack8", code, raise_on_error)
+    n, D, dtype, x_, codes_, exps_ = _rows("fs_seq_unpack8", "pe", x, codes, exps)
+    return _check("fs_seq_unpack8", _typed().fs_seq_unpack8(codes_, exps_, n, D, dtype, x_, _stream()), raise_on_error)
 
 
 def fs_seq_norm_fwd(x, gamma, beta, eps: float, y, mean=None, rstd=None, codes=None, exps=None,
                     raise_on_error: bool = True) -> int:
-    n, D, dtype = _like("fs_seq_norm_fwd", x, same=(y,), columns=(gamma, beta), per_row=(mean, rstd), packed=((codes, exps),))
-    code = _typed().fs_seq_norm_fwd(
-        _ptr(x, _ROWS), n, D, dtype, _ptr(gamma, _F32), _ptr(beta, _F32), eps, _ptr(y, _ROWS), _ptr(mean, _F32),
-        _ptr(rstd, _F32), _ptr(codes, _I8), _ptr(exps, _U8), _stream())
+    n, D, dtype, x_, gamma_, beta_, *rest = _rows("fs_seq_norm_fwd", "ccsrrpe", x, gamma, beta, y, mean, rstd, codes, exps)
+    code = _typed().fs_seq_norm_fwd(x_, n, D, dtype, gamma_, beta_, eps, *rest, _stream())
     return _check("fs_seq_norm_fwd", code, raise_on_error)
 
 
-def _with_workspace(fn: str, call, device, workspace: Optional[torch.Tensor], raise_on_error: bool) -> int:
-    """call(workspace pointer, its size) with the caller's workspace, or one of the size that the entry point asks for."""
+def _with_workspace(fn: str, entry, args: tuple, tail: tuple, device, workspace: Optional[torch.Tensor], raise_on_error: bool) -> int:
+    """entry(*args, workspace, its size, *tail) with the caller's workspace, or one of the size that the entry point asks for."""
     if workspace is None:
-        workspace, size, code = _workspace(call, device)
+        workspace, size, code = _workspace(lambda ws, size: entry(*args, ws, size, *tail), device)
         if code != 0:
             return _check(fn, code, raise_on_error)
     else:
         size = ctypes.c_size_t(workspace.numel() * workspace.element_size())
-    return _check(fn, call(_ptr(workspace), ctypes.byref(size)), raise_on_error)
+    return _check(fn, entry(*args, _ptr(workspace), ctypes.byref(size), *tail), raise_on_error)
 
 
 def fs_seq_norm_bwd(dy, x, mean, rstd, gamma, dx, dgamma, dbeta, workspace: Optional[torch.Tensor] = None,
                     raise_on_error: bool = True) -> int:
-    n, D, dtype = _like("fs_seq_norm_bwd", dy, same=(x, dx), columns=(gamma, dgamma, dbeta), per_row=(mean, rstd))
-    L = _typed()
-    args = (_ptr(dy, _ROWS), _ptr(x, _ROWS), _ptr(mean, _F32), _ptr(rstd, _F32), n, D, dtype, _ptr(gamma, _F32),
-            _ptr(dx, _ROWS), _ptr(dgamma, _F32), _ptr(dbeta, _F32))
-    stream = _stream()
-    return _with_workspace("fs_seq_norm_bwd", lambda ws, size: L.fs_seq_norm_bwd(*args, ws, size, stream), dy.device, workspace,
-                           raise_on_error)
+    n, D, dtype, dy_, x_, mean_, rstd_, *rest = _rows("fs_seq_norm_bwd", "srrcscc", dy, x, mean, rstd, gamma, dx, dgamma, dbeta)
+    return _with_workspace("fs_seq_norm_bwd", _typed().fs_seq_norm_bwd, (dy_, x_, mean_, rstd_, n, D, dtype, *rest), (_stream(),),
+                           dy.device, workspace, raise_on_error)
 
 
 def fs_seq_norm_bwd_packed(dy, codes, exps, mean, rstd, gamma, dx, dgamma, dbeta, workspace: Optional[torch.Tensor] = None,
                            raise_on_error: bool = True) -> int:
-    n, D, dtype = _like("fs_seq_norm_bwd_packed", dy, same=(dx,), columns=(gamma, dgamma, dbeta), per_row=(mean, rstd),
-                        packed=((codes, exps),))
-    L = _typed()
-    args = (_ptr(dy, _ROWS), _ptr(codes, _I8), _ptr(exps, _U8), _ptr(mean, _F32), _ptr(rstd, _F32), n, D, dtype,
-            _ptr(gamma, _F32), _ptr(dx, _ROWS), _ptr(dgamma, _F32), _ptr(dbeta, _F32))
-    stream = _stream()
-    return _with_workspace("fs_seq_norm_bwd_packed", lambda ws, size: L.fs_seq_norm_bwd_packed(*args, ws, size, stream), dy.device,
-                           workspace, raise_on_error)
+    n, D, dtype, dy_, codes_, exps_, mean_, rstd_, *rest = _rows("fs_seq_norm_bwd_packed", "perrcscc", dy, codes, exps, mean, rstd, gamma,
+                                                                 dx, dgamma, dbeta)
+    return _with_workspace("fs_seq_norm_bwd_packed", _typed().fs_seq_norm_bwd_packed,
+                           (dy_, codes_, exps_, mean_, rstd_, n, D, dtype, *rest), (_stream(),), dy.device, workspace, raise_on_error)
 
 
 def seq_norm_bwd_workspace_bytes(n: int, D: int, dtype: int) -> int:
+    """The packed form needs the same."""
     size = ctypes.c_size_t(0)
     code = _typed().fs_seq_norm_bwd(None, None, None, None, n, D, dtype, None, None, None, None, None, ctypes.byref(size), None)
     _check("fs_seq_norm_bwd", code, True)
     return int(size.value)
 
 
-def _sequences(fn: str, rows, offsets, T: int, B: int, states) -> None:
-    """offsets[T*B + 1] and the [T*B, D] float32 states at the sequences' ends, on the device of the rows."""
-    where = rows.get_device()
-    if offsets.dim() != 1 or offsets.shape[0] != T * B + 1 or offsets.get_device() != where:
-        raise ValueError(f"{fn}: expected {T * B + 1} offsets on the device of the rows, got {tuple(offsets.shape)} on {offsets.device}")
-    for t in states:
-        if t is not None and (tuple(t.shape) != (T * B, rows.shape[1]) or t.get_device() != where):
-            raise ValueError(f"{fn}: states are [{T * B}, {rows.shape[1]}] on the device of the rows, got {tuple(t.shape)} on {t.device}")
-
-
 def fs_seq_scan_fwd(x, gate, offsets, T: int, B: int, h0, h, h_last=None, dev_status=None,
                     workspace: Optional[torch.Tensor] = None, raise_on_error: bool = True) -> int:
-    n, D, dtype = _like("fs_seq_scan_fwd", x, same=(gate, h))
-    _sequences("fs_seq_scan_fwd", x, offsets, T, B, (h0, h_last))
-    L = _typed()
-    args = (_ptr(x, _ROWS), _ptr(gate, _ROWS), n, D, dtype, _ptr(offsets, _I64), T, B, _ptr(h0, _F32), _ptr(h, _ROWS),
-            _ptr(h_last, _F32))
-    tail = (_stream(), _ptr(dev_status, _I32))
-    return _with_workspace("fs_seq_scan_fwd", lambda ws, size: L.fs_seq_scan_fwd(*args, ws, size, *tail), x.device, workspace,
-                           raise_on_error)
+    n, D, dtype, x_, gate_, offsets_, h0_, h_, last_ = _rows("fs_seq_scan_fwd", "sotst", x, gate, offsets, h0, h, h_last, sequences=T * B)
+    return _with_workspace("fs_seq_scan_fwd", _typed().fs_seq_scan_fwd, (x_, gate_, n, D, dtype, offsets_, T, B, h0_, h_, last_),
+                           (_stream(), _ptr(dev_status, _I32)), x.device, workspace, raise_on_error)
 
 
 def fs_seq_scan_bwd(dh, dh_last, x, gate, h, offsets, T: int, B: int, h0, dx, dgate, dh0=None, dev_status=None,
                     workspace: Optional[torch.Tensor] = None, raise_on_error: bool = True) -> int:
-    n, D, dtype = _like("fs_seq_scan_bwd", dh, same=(x, gate, h, dx, dgate))
-    _sequences("fs_seq_scan_bwd", dh, offsets, T, B, (dh_last, h0, dh0))
-    L = _typed()
-    args = (_ptr(dh, _ROWS), _ptr(dh_last, _F32), _ptr(x, _ROWS), _ptr(gate, _ROWS), _ptr(h, _ROWS), n, D, dtype,
-            _ptr(offsets, _I64), T, B, _ptr(h0, _F32), _ptr(dx, _ROWS), _ptr(dgate, _ROWS), _ptr(dh0, _F32))
-    tail = (_stream(), _ptr(dev_status, _I32))
-    return _with_workspace("fs_seq_scan_bwd", lambda ws, size: L.fs_seq_scan_bwd(*args, ws, size, *tail), dh.device, workspace,
-                           raise_on_error)
+    n, D, dtype, dh_, last_, x_, gate_, h_, offsets_, *rest = _rows("fs_seq_scan_bwd", "tsssotsst", dh, dh_last, x, gate, h, offsets, h0, dx, dgate,
+                                                                    dh0, sequences=T * B)
+    return _with_workspace("fs_seq_scan_bwd", _typed().fs_seq_scan_bwd, (dh_, last_, x_, gate_, h_, n, D, dtype, offsets_, T, B, *rest),
+                           (_stream(), _ptr(dev_status, _I32)), dh.device, workspace, raise_on_error)
 
 
 def fs_seq_scan_bwd_packed(dh, dh_last, x_codes, x_exps, gate_codes, gate_exps, h_codes, h_exps, offsets, T: int, B: int,
                            h0, dx, dgate, dh0=None, dev_status=None, workspace: Optional[torch.Tensor] = None,
                            raise_on_error: bool = True) -> int:
-    n, D, dtype = _like("fs_seq_scan_bwd_packed", dh, same=(dx, dgate),
-                        packed=((x_codes, x_exps), (gate_codes, gate_exps), (h_codes, h_exps)))
-    _sequences("fs_seq_scan_bwd_packed", dh, offsets, T, B, (dh_last, h0, dh0))
-    L = _typed()
-    args = (_ptr(dh, _ROWS), _ptr(dh_last, _F32), _ptr(x_codes, _I8), _ptr(x_exps, _U8), _ptr(gate_codes, _I8),
-            _ptr(gate_exps, _U8), _ptr(h_codes, _I8), _ptr(h_exps, _U8), n, D, dtype, _ptr(offsets, _I64), T, B,
-            _ptr(h0, _F32), _ptr(dx, _ROWS), _ptr(dgate, _ROWS), _ptr(dh0, _F32))
-    tail = (_stream(), _ptr(dev_status, _I32))
-    return _with_workspace("fs_seq_scan_bwd_packed", lambda ws, size: L.fs_seq_scan_bwd_packed(*args, ws, size, *tail), dh.device,
-                           workspace, raise_on_error)
+    n, D, dtype, *got = _rows("fs_seq_scan_bwd_packed", "tpepepeotsst", dh, dh_last, x_codes, x_exps, gate_codes, gate_exps, h_codes, h_exps,
+                              offsets, h0, dx, dgate, dh0, sequences=T * B)
+    return _with_workspace("fs_seq_scan_bwd_packed", _typed().fs_seq_scan_bwd_packed, (*got[:8], n, D, dtype, got[8], T, B, *got[9:]),
+                           (_stream(), _ptr(dev_status, _I32)), dh.device, workspace, raise_on_error)
 
 
 def seq_scan_fwd_workspace_bytes(n: int, D: int, dtype: int, T: int, B: int) -> int:
@@ -681,10 +649,8 @@ def seq_scan_bwd_workspace_bytes(n: int, D: int, dtype: int, T: int, B: int) -> 
 
 
 def fs_seq_scan_step(x, gate, state, state_out, h, raise_on_error: bool = True) -> int:
-    n, D, dtype = _like("fs_seq_scan_step", x, same=(gate, h), float_rows=(state, state_out))
-    code = _typed().fs_seq_scan_step(_ptr(x, _ROWS), _ptr(gate, _ROWS), n, D, dtype, _ptr(state, _F32), _ptr(state_out, _F32),
-                                     _ptr(h, _ROWS), _stream())
-    return _check("fs_seq_scan_step", code, raise_on_error)
+    n, D, dtype, x_, gate_, *rest = _rows("fs_seq_scan_step", "sffs", x, gate, state, state_out, h)
+    return _check("fs_seq_scan_step", _typed().fs_seq_scan_step(x_, gate_, n, D, dtype, *rest, _stream()), raise_on_error)
 
 
 class CostParams(ctypes.Structure):

@@ -342,3 +342,38 @@ def test_step_in_place(dtype):
     fs.fs_seq_scan_step(x, gate, state, out, h)
     fs.fs_seq_scan_step(x, gate, state, state, x)
     assert same_bits(x, h) and same_bits(state, out)
+
+
+def test_the_binding_in_native_code_and_in_python():
+    """The native look at the tensors and the one in Python give the same sizes and pointers, and refuse the same."""
+    x = torch.zeros(6, 72, device=DEV, dtype=torch.bfloat16)
+    good = dict(s=torch.empty_like(x), f=torch.empty(6, 72, device=DEV), c=torch.empty(72, device=DEV), r=torch.empty(6, device=DEV),
+                p=torch.empty(6, 72, device=DEV, dtype=torch.int8), e=torch.empty(6, 3, device=DEV, dtype=torch.uint8),
+                o=torch.zeros(4, device=DEV, dtype=torch.int64), t=torch.empty(3, 72, device=DEV))
+    kinds = "".join(good)
+    assert fs._fit is not None
+    for tensors in (tuple(good.values()), (None,) * 8):
+        assert fs._fit(kinds, 0, 3, x, *tensors) == fs._rows_checked("test", kinds, x, tensors, 3)
+
+    class Sub(torch.Tensor):
+        pass
+
+    for k, t in good.items():
+        bad = [t[1:], t.cpu(), t.to(torch.float64), t.unsqueeze(0), t.reshape(-1)[:-1], t[..., ::2]]
+        if t.dim() > 1:
+            bad += [t[:, 1:], t.t()]
+        for b in bad:
+            args = [b if k == j else None for j in good]
+            assert fs._fit(kinds, 0, 3, x, *args) is None, (k, tuple(b.shape))
+            with pytest.raises((ValueError, TypeError)):
+                fs._rows_checked("test", kinds, x, tuple(args), 3)
+    wide = torch.zeros(6, 144, device=DEV, dtype=torch.bfloat16)[:, :72]               # the right sizes, rows apart
+    for args in ((x, wide), (wide, x)):
+        assert fs._fit("s", 0, 0, *args) is None
+        with pytest.raises(TypeError):
+            fs._rows_checked("test", "s", args[0], args[1:], 0)
+    assert fs._fit("s", 1, 0, x, x) is None and fs._fit("ss", 0, 0, x, x) is None and fs._fit("?", 0, 0, x, x) is None
+    assert fs._fit("s", 0, 0, x, "text") is None and fs._fit("s", 0, 0, 7, x) is None and fs._fit() is None
+    assert fs._fit("s", 0, 0, x.as_subclass(Sub), x) is None                            # Python's to look at
+    assert fs._rows("test", "s", x.as_subclass(Sub), x) == fs._rows("test", "s", x, x)
+    assert fs._rows("test", "s", torch.nn.Parameter(x), x)[3] == x.data_ptr()
