@@ -85,7 +85,7 @@ __device__ __forceinline__ T* piece_at(T* p, uint32_t at)
 
 // Rows of whole cache lines are read once by one instruction each and streamed past the caches; of other rows a line belongs
 // to two, and to instructions apart in time, so they go through the caches (us, streamed : cached: 4.2 M rows of 256 bytes
-// forward 620 : 653, backward 1217 : 1301; of 272 bytes forward 769 : 753; of 48 bytes backward 557 : 412).
+// forward 547 : 588, backward 1102 : 1192; of 272 bytes forward 721 : 676; of 48 bytes backward 484 : 343).
 template <bool STREAM, typename T>
 __device__ __forceinline__ T load_rows(const T* p)
 {
@@ -621,12 +621,12 @@ __global__ __launch_bounds__(kBlock, 2) void scan_bwd_kernel(ScanArgs a, const i
     const int cb = (int)(t % (uint32_t)a.col_blocks);
     if (k < a.tiles) {
         const Place<Shape> p(a, tile, a.tiles - 1 - k, cb);
-                const Bounds bounds(a, tile_seq == nullptr ? 0 : tile_seq[a.tiles - 1 - k]);
+        const Bounds bounds(a, tile_seq == nullptr ? 0 : tile_seq[a.tiles - 1 - k]);
         const u32x4* from_d = a.dh + p.row0 * a.units;
         u32x4 raw_d[R];
         Saved<DT, PACKED, 0, (G > 0)> x[R];
         Saved<DT, PACKED, 1, (G > 0)> gate[R];
-        Saved<DT, PACKED, 2, (G > 0)> before[R];                 // h of the row before
+        Saved<DT, PACKED, 2, (G > 0)> before[R];        // h of the row before
 #pragma unroll
         for (int r = R - 1; r >= 0; --r) {              // in the order of their use
             const uint32_t block = p.row(r) * (uint32_t)a.nb + p.own / LPB;
@@ -737,8 +737,8 @@ __global__ __launch_bounds__(kBlock) void scan_clear_kernel(ScanArgs a, int64_t 
     a.tile_seq[i] = (int32_t)lo;
 }
 
-// (No pointer is restricted: h may be x, state_out state.)
-// One token of every session: a 16-byte piece of x, gate and out to a lane, its states as fp32 beside it.
+// One token of every session: a 16-byte piece of x, gate and h to a lane, its states as fp32 beside it.  (No pointer is
+// restricted: h may be x, state_out state.)
 template <int DT>
 __global__ __launch_bounds__(kBlock) void scan_step_kernel(const u32x4* x, const u32x4* gate, const float* state,
                                                            float* state_out, u32x4* h, int64_t pieces)
@@ -781,10 +781,9 @@ int scan_lanes(int units, int N)
 constexpr int kMostPieces = (1 << 18) - 1;
 
 // Values of a lane, R rows of a 16-byte piece.  Forward f and b of 64 values are 128 registers of the 168 with which three
-// workgroups share a CU (32 values, four workgroups: 863 us instead of 544 for 4.2 M rows of 128 fp16; 128 values, two: 753): longer
+// workgroups share a CU (32 values, four workgroups: 867 us instead of 547 for 4.2 M rows of 128 fp16; 128 values, two: 753): longer
 // tiles mean fewer words, counters and searches a row.  Backward five numbers a value are held, f, 1 - f, dh and, as they came, x
-// and h: 32 values (64: 1208 us instead of 1098 in bf16, 1446 instead of 1025 for half as many rows of fp32; 16: 1754 instead of
-// 1317 when that was measured).
+// and h: 32 values (64: 1208 us instead of 1100 in bf16, 1489 instead of 1024 for half as many rows of fp32; 16: 1720 and 1047).
 constexpr int kFwdValues = 64, kBwdValues = 32;
 
 // Everything that follows from the sizes; *a gets them, `words` the workspace's places.
