@@ -603,10 +603,10 @@ fs_status fs_seq_unpack8(
  * fs_seq_norm_bwd_packed -- the same with x given as a checkpoint (codes, exps
  *   of fs_seq_pack8 or fs_seq_norm_fwd); mean and rstd are those of the rows
  *   themselves.
- *   Host faults: unknown dtype; n < 0, n >= 2^31, D < 1 (FS_ERR_SIZE); eps not
- *   positive and finite (FS_ERR_CONFIG); NULL; alignment as above, gamma and
- *   beta 16-byte aligned too; workspace as everywhere.  n == 0: the backward
- *   pass writes zeros to dgamma and dbeta.
+ *   Host faults: unknown dtype; n < 0, n >= 2^31, D < 1, a row of 4 MB or more
+ *   (FS_ERR_SIZE); eps not positive and finite (FS_ERR_CONFIG); NULL; alignment
+ *   as above, gamma and beta 16-byte aligned too; workspace as everywhere.
+ *   n == 0: the backward pass writes zeros to dgamma and dbeta.
  */
 fs_status fs_seq_norm_fwd(
     const void* x, int64_t n, int32_t D, fs_dtype dtype, const float* gamma, const float* beta, float eps,

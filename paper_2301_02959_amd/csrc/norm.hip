@@ -565,6 +565,7 @@ fs_status norm_bwd(NormArgs a, bool packed, int32_t D, fs_dtype dtype, float* dg
     if (!workspace_bytes) return FS_ERR_NULL;
     const fs_status st = check_seq_rows(a.n, D, dtype, &a.units);
     if (st != FS_OK) return st;
+    if (a.units > kMostPieces) return FS_ERR_SIZE;
     Carver ws(workspace);
     const int64_t blocks = bwd_blocks(a.n, a.units);
     a.partial = ws.take<float>((size_t)(blocks > 0 ? blocks : 1) * 2 * (size_t)D);      // never nothing: a null workspace is a question
@@ -608,6 +609,7 @@ extern "C" fs_status fs_seq_norm_fwd(
     NormArgs a = {};
     const fs_status st = check_seq_rows(n, D, dtype, &a.units);
     if (st != FS_OK) return st;
+    if (a.units > kMostPieces) return FS_ERR_SIZE;
     if (!(eps > 0.0f) || __builtin_isinf(eps)) return FS_ERR_CONFIG;
     if (n == 0) return FS_OK;
     if (!x || !gamma || !beta || !y) return FS_ERR_NULL;

@@ -777,9 +777,6 @@ int scan_lanes(int units, int N)
     return (units + blocks - 1) / blocks;
 }
 
-// Longest row, in 16-byte pieces (4 MB): a tile of at most 1024 rows is addressed by 32-bit offsets in bytes.
-constexpr int kMostPieces = (1 << 18) - 1;
-
 // Values of a lane, R rows of a 16-byte piece.  Forward f and b of 64 values are 128 registers of the 168 with which three
 // workgroups share a CU (32 values, four workgroups: 867 us instead of 547 for 4.2 M rows of 128 fp16; 128 values, two: 753): longer
 // tiles mean fewer words, counters and searches a row.  Backward five numbers a value are held, f, 1 - f, dh and, as they came, x
@@ -792,7 +789,7 @@ fs_status plan_scan(int64_t n, int32_t D, fs_dtype dtype, int32_t T, int32_t B, 
     const fs_status st = check_seq_rows(n, D, dtype, &a->units);
     if (st != FS_OK) return st;
     if (T < 1 || B < 1 || (int64_t)T * B >= (1LL << 31)) return FS_ERR_SIZE;
-    if (a->units > kMostPieces) return FS_ERR_SIZE;
+    if (a->units > kMostPieces) return FS_ERR_SIZE;                 // a tile of at most 1024 rows has 32-bit offsets in bytes
     a->S = (int64_t)T * B;
     a->n = n;
     a->nb = (int)pack_blocks(D);

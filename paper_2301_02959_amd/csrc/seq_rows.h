@@ -56,6 +56,10 @@ __device__ __forceinline__ float group_sum(float v)
 // A launch has fewer than 2^32 threads: the most workgroups of kBlock.  Longer batches go in several launches of whole rows.
 constexpr int64_t kMostGrid = (1LL << 32) / kBlock - 1;
 
+// Longest row of the norm and the recurrence, in 16-byte pieces (4 MB): the norm's launches over the columns stay under
+// kMostGrid and its sums in fp32 of a use, the recurrence's tiles within 32-bit offsets.
+constexpr int kMostPieces = (1 << 18) - 1;
+
 inline bool misaligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
 
 // Sizes and type of n rows of D elements; *units = 16-byte pieces of a row.

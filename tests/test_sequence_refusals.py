@@ -145,3 +145,13 @@ def test_a_workspace_is_never_of_no_bytes(name, n):
     asked = ctypes.c_size_t(0)
     assert call(name, *dict(BASE[name], n=n, ws=None, size=ctypes.byref(asked)).values()) == 0
     assert asked.value >= 4
+
+
+@pytest.mark.parametrize("name", sorted(k for k in BASE if "norm" in k or "scan_fwd" in k or "scan_bwd" in k))
+def test_rows_of_four_megabytes_and_more(name):
+    """Rows so long that a launch over their columns or an offset inside a tile would leave its range."""
+    change = {"ws": None} if "size" in BASE[name] else {"n": 0}
+    for dtype, D in ((0, 1 << 20), (1, 1 << 21), (2, 1 << 21), (0, 1 << 26), (2, (1 << 31) - 8)):
+        assert run(name, dtype=dtype, D=D, **change) == SIZE
+    for dtype, D in ((0, (1 << 20) - 4), (2, (1 << 21) - 8)):
+        assert run(name, dtype=dtype, D=D, **change) == 0
