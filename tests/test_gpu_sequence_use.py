@@ -377,3 +377,24 @@ def test_the_binding_in_native_code_and_in_python():
     assert fs._fit("s", 0, 0, x.as_subclass(Sub), x) is None                            # Python's to look at
     assert fs._rows("test", "s", x.as_subclass(Sub), x) == fs._rows("test", "s", x, x)
     assert fs._rows("test", "s", torch.nn.Parameter(x), x)[3] == x.data_ptr()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_the_longest_rows(dtype):
+    """One 16-byte piece under 4 MB a row."""
+    D = width((1 << 18) - 1, dtype)
+    check_norm(2, D, dtype, 18)
+    check_scan([1, 0, 2], D, dtype, 18)
+
+
+def test_a_checkpoint_of_one_row_of_any_length():
+    """A flat tensor as one row: the codes of the same values in many rows of whole blocks."""
+    n, D = 1 << 12, 1 << 15
+    x = torch.empty(n, D, dtype=torch.bfloat16, device=DEV).normal_()
+    codes, exps = pack(x)
+    flat, flat_exps = pack(x.view(1, -1))
+    assert torch.equal(flat.view(n, D), codes) and torch.equal(flat_exps.view(n, -1), exps)
+    back, flat_back = torch.empty_like(x), torch.empty_like(x)
+    fs.fs_seq_unpack8(codes, exps, back)
+    fs.fs_seq_unpack8(flat, flat_exps, flat_back.view(1, -1))
+    assert same_bits(back, flat_back)
