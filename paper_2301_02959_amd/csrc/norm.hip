@@ -12,7 +12,7 @@
 // LDS and writes one partial row, norm_grad_sum adds the partial rows in their order: no atomics, the same bits every run.
 //
 // Measured, 3.93 M rows of 256 bf16 (us, TB/s of what has to be read and written): forward 691 (5.8), with the checkpoint
-// written too 884 (5.7), backward 1078 (5.6), from the checkpoint 930 (5.4).
+// written too 884 (5.7), backward 1078 (5.6), from the checkpoint 890 (5.7).
 #include "pack8.h"
 #include "seq_rows.h"
 
@@ -128,8 +128,10 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_kernel(NormArgs a)
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             Piece<DT>::unpack(raw[u][p], c[p]);
+            float t = 0.0f;                              // (a piece's sum of its own: shorter chains of roundings)
 #pragma unroll
-            for (int i = 0; i < N; ++i) s += c[p][i];
+            for (int i = 0; i < N; ++i) t += c[p][i];
+            s += t;
             if constexpr (PACK) write_codes<DT, G>(a, row, lig + p * G, row < a.n && lig + p * G < a.units, c[p]);
         }
         float mean = row_sum<G>(s, lds) * a.inv_D;
@@ -137,12 +139,15 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_kernel(NormArgs a)
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const bool in = lig + p * G < a.units;
+            float t1 = 0.0f, t2 = 0.0f;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 c[p][i] = in ? c[p][i] - mean : 0.0f;
-                s1 += c[p][i];
-                s2 = fmaf(c[p][i], c[p][i], s2);
+                t1 += c[p][i];
+                t2 = fmaf(c[p][i], c[p][i], t2);
             }
+            s1 += t1;
+            s2 += t2;
         }
         const float off = row_sum<G>(s1, lds) * a.inv_D;
         const float var = fmaf(-off, off, row_sum<G>(s2, lds) * a.inv_D);
@@ -287,7 +292,7 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_kernel(NormArgs a)
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 const bool in = row < a.n && lig + p * G < a.units;
-                float dy[N];
+                float dy[N], t1 = 0.0f, t2 = 0.0f;
                 x_raw[u][p].values(w[p]);
                 Piece<DT>::unpack(dy_raw[u][p], dy);
 #pragma unroll
@@ -298,9 +303,11 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_kernel(NormArgs a)
                         db[p][i] += dy[i];
                     }
                     g[p][i] = dy[i] * gamma[p][i];
-                    s1 += g[p][i];
-                    s2 = fmaf(g[p][i], w[p][i], s2);
+                    t1 += g[p][i];
+                    t2 = fmaf(g[p][i], w[p][i], t2);
                 }
+                s1 += t1;
+                s2 += t2;
             }
             if (!writes) continue;
             const float m1 = row_sum<G>(s1, sums) * a.inv_D, m2 = row_sum<G>(s2, sums) * a.inv_D;
@@ -450,7 +457,10 @@ constexpr int kWideChunks = 64;              // row chunks of the wide columns' 
 constexpr int kSmallRounds = 8;              // rounds of one workgroup over all rows that are worth a launch less (100 rows of 256: 6.9 us, with the second launch 10.8)
 
 // Lanes (G) and pieces a lane (P) of a row as constants: CALL(G, P).  Up to 256 pieces a wave or a part of it has the row, up
-// to 1024 the workgroup.
+// to 1024 the workgroup.  One piece a lane where a wave's instruction then takes whole rows one after the other; with three pieces a
+// lane fewer lanes lie past the row's end, and rows of more instructions apart in time share more cache lines.  Bf16, 0.8 GB, us:
+// forward rows of 40 pieces (64, 1) 313, (16, 3) 265; 150 (64, 4) 473, (64, 3) 292; 600 (256, 4) 342, (256, 3) 287; but 17
+// (32, 1) 342, (8, 3) 476.
 #define FS_DISPATCH_ROW(units, CALL)                                                    \
     do {                                                                                \
         if ((units) > 512) { CALL(256, 4); }                                            \
@@ -463,27 +473,54 @@ constexpr int kSmallRounds = 8;              // rounds of one workgroup over all
         else if ((units) > 4) { CALL(8, 1); }                                           \
         else { CALL(4, 1); }                                                            \
     } while (0)
+#define FS_DISPATCH_FWD_ROW(units, CALL)                                                \
+    do {                                                                                \
+        if ((units) > 512 && (units) <= 768) { CALL(256, 3); }                          \
+        else if ((units) > 128 && (units) <= 192) { CALL(64, 3); }                      \
+        else if ((units) > 32 && (units) <= 48) { CALL(16, 3); }                        \
+        else FS_DISPATCH_ROW(units, CALL);                                              \
+    } while (0)
+// Backward fewer lanes a row still: what a lane does beside its columns (the sums over the lanes, the row's statistics and
+// places) is shared by more of them.  From the checkpoint, bf16, 0.4 G values, us: 40 pieces (64, 1) 562, (16, 3) 346; 64 (64, 1) 377,
+// (32, 2) 353; 65 (64, 2) 589, (32, 3) 413; 100 (64, 2) 408, (32, 4) 354; 513 (256, 4) 523, (256, 3) 449; from the rows 1 to 11 %.
+// few: rows of 16-bit types from their checkpoint, which have the most to do for a byte: 9 pieces (16, 1) 600, (8, 2) 563; 24
+// (32, 1) 463, (8, 3) 355; 32 (32, 1) 933, (16, 2) 890 (3.93 M rows).  From the rows 17 pieces (32, 1) 488, (16, 2) 540, and of fp32 from
+// its checkpoint (32, 1) 432, (8, 3) 479.
+#define FS_DISPATCH_BWD_ROW(units, few, CALL)                                           \
+    do {                                                                                \
+        if ((units) > 512 && (units) <= 768) { CALL(256, 3); }                          \
+        else if ((units) > 96 && (units) <= 128) { CALL(32, 4); }                       \
+        else if ((units) > 64 && (units) <= 96) { CALL(32, 3); }                        \
+        else if ((units) > 48 && (units) <= 64) { CALL(32, 2); }                        \
+        else if ((units) > 32 && (units) <= 48) { CALL(16, 3); }                        \
+        else if ((few) && (units) > 24 && (units) <= 32) { CALL(16, 2); }               \
+        else if ((few) && (units) > 16 && (units) <= 24) { CALL(8, 3); }                \
+        else if ((few) && (units) > 8 && (units) <= 16) { CALL(8, 2); }                 \
+        else FS_DISPATCH_ROW(units, CALL);                                              \
+    } while (0)
 
-// Rows that a group has in flight (3.93 M rows of 256 bf16, us: forward 1, 2, 4, 8 rows 728, 691, 718, 718; backward 2, 4 rows 1114, 1078).
-constexpr int fwd_rows(int P) { return P == 4 ? 1 : 2; }
-constexpr int bwd_rows(int P) { return P == 1 ? 4 : 1; }
+// Rows that a group has in flight.  Forward 2 (3.93 M rows of 256 bf16: 1, 2, 4, 8 rows 728, 691, 718, 718 us; rows of 1024 pieces 1, 2
+// rows 339, 280).  Backward 4 of one piece a lane (3.93 M rows of 256: 2, 4 rows 1114, 1078), 2 of a workgroup with two pieces (300
+// pieces: 1, 2 rows 544, 472), else 1 (80 pieces, three a lane: 1, 2 rows 411, 434).
+constexpr int kFwdRows = 2;
+constexpr int bwd_rows(int G, int P) { return P == 1 ? 4 : G > kWave && P == 2 ? 2 : 1; }
 
 // Rows of a workgroup's round in the backward pass.
-int64_t bwd_round(int units)
+int64_t bwd_round(int units, bool few)
 {
-#define CALL(G, P) return (int64_t)(kBlock / G) * bwd_rows(P)
-    FS_DISPATCH_ROW(units, CALL);
+#define CALL(G, P) return (int64_t)(kBlock / G) * bwd_rows(G, P)
+    FS_DISPATCH_BWD_ROW(units, few, CALL);
 #undef CALL
 }
 
-int64_t bwd_blocks(int64_t n, int units)
+int64_t bwd_blocks(int64_t n, int units, bool few)
 {
     if (units > kWidePieces) return n < kWideChunks ? n : kWideChunks;
-    const int64_t per = bwd_round(units), need = (n + per - 1) / per;
+    const int64_t per = bwd_round(units, few), need = (n + per - 1) / per;
     return need < kBwdBlocks ? need : kBwdBlocks;
 }
 
-bool bwd_small(int64_t n, int units) { return units <= kWidePieces && n <= kSmallRounds * bwd_round(units); }
+bool bwd_small(int64_t n, int units, bool few) { return units <= kWidePieces && n <= kSmallRounds * bwd_round(units, few); }
 
 // The arguments from row r0 on, for `rows` rows.
 template <int DT>
@@ -503,8 +540,8 @@ NormArgs part_of(NormArgs a, int64_t r0, int64_t rows)
 int64_t fwd_launch_rows(int units)
 {
     if (units > kWidePieces) return kMostGrid;
-#define CALL(G, P) return kMostGrid * ((kBlock / G) * fwd_rows(P))
-    FS_DISPATCH_ROW(units, CALL);
+#define CALL(G, P) return kMostGrid * ((kBlock / G) * kFwdRows)
+    FS_DISPATCH_FWD_ROW(units, CALL);
 #undef CALL
 }
 
@@ -524,12 +561,12 @@ fs_status norm_fwd_launch(const NormArgs& a, hipStream_t s)
     }
 #define CALL(G, P)                                                                                                        \
     do {                                                                                                                  \
-        constexpr int U = fwd_rows(P);                                                                                    \
+        constexpr int U = kFwdRows;                                                                                       \
         const unsigned grid = (unsigned)((a.n + (kBlock / G) * U - 1) / ((kBlock / G) * U));                              \
         if (pack) FS_LAUNCH("norm_fwd", (norm_fwd_kernel<DT, G, P, U, true>), dim3(grid), dim3(kBlock), s, a);            \
         else FS_LAUNCH("norm_fwd", (norm_fwd_kernel<DT, G, P, U, false>), dim3(grid), dim3(kBlock), s, a);                \
     } while (0)
-    FS_DISPATCH_ROW(a.units, CALL);
+    FS_DISPATCH_FWD_ROW(a.units, CALL);
 #undef CALL
     return FS_OK;
 }
@@ -537,7 +574,8 @@ fs_status norm_fwd_launch(const NormArgs& a, hipStream_t s)
 template <int DT, bool PACKED>
 fs_status norm_bwd_launch(const NormArgs& a, hipStream_t s)
 {
-    const unsigned blocks = (unsigned)bwd_blocks(a.n, a.units);
+    constexpr bool few = PACKED && DT != FS_F32;
+    const unsigned blocks = (unsigned)bwd_blocks(a.n, a.units, few);
     if (a.units > kWidePieces) {
         // the sums first: dx may be dy
         FS_LAUNCH("norm_cols_wide", (norm_cols_wide_kernel<DT, PACKED>), dim3((unsigned)((a.units + kBlock - 1) / kBlock), blocks),
@@ -550,11 +588,11 @@ fs_status norm_bwd_launch(const NormArgs& a, hipStream_t s)
     }
 #define CALL(G, P)                                                                                                        \
     do {                                                                                                                  \
-        constexpr int U = bwd_rows(P);                                                                                    \
-        if (bwd_small(a.n, a.units)) FS_LAUNCH("norm_bwd", (norm_bwd_kernel<DT, G, P, U, PACKED, true>), dim3(a.dx == a.dy ? 1 : blocks + 1), dim3(kBlock), s, a); \
+        constexpr int U = bwd_rows(G, P);                                                                                 \
+        if (bwd_small(a.n, a.units, few)) FS_LAUNCH("norm_bwd", (norm_bwd_kernel<DT, G, P, U, PACKED, true>), dim3(a.dx == a.dy ? 1 : blocks + 1), dim3(kBlock), s, a); \
         else FS_LAUNCH("norm_bwd", (norm_bwd_kernel<DT, G, P, U, PACKED, false>), dim3(blocks), dim3(kBlock), s, a);      \
     } while (0)
-    FS_DISPATCH_ROW(a.units, CALL);
+    FS_DISPATCH_BWD_ROW(a.units, few, CALL);
 #undef CALL
     return FS_OK;
 }
@@ -567,8 +605,10 @@ fs_status norm_bwd(NormArgs a, bool packed, int32_t D, fs_dtype dtype, float* dg
     if (st != FS_OK) return st;
     if (a.units > kMostPieces) return FS_ERR_SIZE;
     Carver ws(workspace);
-    const int64_t blocks = bwd_blocks(a.n, a.units);
-    a.partial = ws.take<float>((size_t)(blocks > 0 ? blocks : 1) * 2 * (size_t)D);      // never nothing: a null workspace is a question
+    const bool few = packed && dtype != FS_F32;
+    const int64_t blocks = bwd_blocks(a.n, a.units, few), other = bwd_blocks(a.n, a.units, !few);      // one size for both forms
+    const int64_t held = blocks > other ? blocks : other;
+    a.partial = ws.take<float>((size_t)(held > 0 ? held : 1) * 2 * (size_t)D);      // never nothing: a null workspace is a question
     if (!workspace) { *workspace_bytes = ws.used; return FS_OK; }
     if (*workspace_bytes < ws.used || misaligned(workspace, 256)) return FS_ERR_WORKSPACE;
     if (!a.gamma || !dgamma || !dbeta) return FS_ERR_NULL;
@@ -591,7 +631,7 @@ fs_status norm_bwd(NormArgs a, bool packed, int32_t D, fs_dtype dtype, float* dg
             FS_DISPATCH_DTYPE(dtype, CALL)
 #undef CALL
         }
-        if (rc != FS_OK || bwd_small(a.n, a.units)) return rc;
+        if (rc != FS_OK || bwd_small(a.n, a.units, few)) return rc;
     }
     FS_LAUNCH("norm_grad_sum", norm_grad_sum_kernel, dim3((unsigned)((2 * (int64_t)D + kSumCols - 1) / kSumCols)),
               dim3(kSumCols * kSumRows), s, a.partial, (int)blocks, (int64_t)D, dgamma, dbeta);

@@ -398,3 +398,33 @@ def test_a_checkpoint_of_one_row_of_any_length():
     fs.fs_seq_unpack8(codes, exps, back)
     fs.fs_seq_unpack8(flat, flat_exps, flat_back.view(1, -1))
     assert same_bits(back, flat_back)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("units", [9, 13, 16, 17, 24, 25, 32, 40, 48, 49, 64, 65, 96, 97, 128, 150, 192, 193, 300, 512, 513, 768, 769])
+def test_norm_either_side_of_every_layout(dtype, units):
+    """Widths at which the lanes and pieces of a row change, in one launch and in two."""
+    check_norm(5, width(units, dtype), dtype, units)
+    check_norm(561, width(units, dtype), dtype, units)
+
+
+def test_either_form_takes_the_others_workspace():
+    """seq_norm_bwd_workspace_bytes holds for the packed form, whatever rows a workgroup of either takes at a time."""
+    for dtype, kind in ((torch.float32, fs.FS_F32), (torch.float16, fs.FS_F16), (torch.bfloat16, fs.FS_BF16)):
+        for units in (9, 24, 32, 40, 600, 1100):
+            for n in (1, 100, 150, 3000):
+                D = width(units, dtype)
+                gen = generator(units + n)
+                x, dy = rows(gen, n, D, dtype), rows(gen, n, D, dtype)
+                gamma = torch.ones(D, device=DEV)
+                mean, rstd = torch.zeros(n, device=DEV), torch.ones(n, device=DEV)
+                codes, exps = pack(x)
+                ws = torch.empty(fs.seq_norm_bwd_workspace_bytes(n, D, kind), dtype=torch.uint8, device=DEV)
+                out = [torch.empty_like(x), torch.empty(D, device=DEV), torch.empty(D, device=DEV)]
+                alone = [torch.empty_like(t) for t in out]
+                fs.fs_seq_norm_bwd_packed(dy, codes, exps, mean, rstd, gamma, *out, workspace=ws)
+                fs.fs_seq_norm_bwd_packed(dy, codes, exps, mean, rstd, gamma, *alone)
+                assert all(same_bits(a, b) for a, b in zip(out, alone))
+                fs.fs_seq_norm_bwd(dy, x, mean, rstd, gamma, *out, workspace=ws)
+                # dbeta does not depend on x: n additions in either order
+                assert torch.allclose(out[2], alone[2], rtol=0, atol=2 * n * 2.0 ** -24 * float(dy.float().abs().sum(0).max()))
