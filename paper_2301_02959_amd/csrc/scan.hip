@@ -85,7 +85,7 @@ __device__ __forceinline__ T* piece_at(T* p, uint32_t at)
 
 // Rows of whole cache lines are read once by one instruction each and streamed past the caches; of other rows a line belongs
 // to two, and to instructions apart in time, so they go through the caches (us, streamed : cached: 4.2 M rows of 256 bytes
-// forward 547 : 588, backward 1102 : 1192; of 272 bytes forward 721 : 676; of 48 bytes backward 484 : 343).
+// forward 547 : 588, backward 1102 : 1192; of 272 bytes 725 : 677 and 1508 : 1387; of 48 bytes backward 538 : 283).
 template <bool STREAM, typename T>
 __device__ __forceinline__ T load_rows(const T* p)
 {
@@ -131,11 +131,16 @@ struct Saved {
     }
 };
 
+// Most groups of a workgroup: all its threads have one from 16-bit rows of two pieces on (against 64 groups, 4.2 M rows of 8, 16 and 24
+// bf16, us: forward 101 : 128, 117 : 139, 173 : 173).  fp32 groups have twice the rows: their marks' LDS would cost a workgroup a CU
+// (rows of 12: 170 : 162).  Backward 154 : 221, 204 : 250, 283 : 292.
+constexpr __host__ __device__ int most_groups(int N) { return N == 8 ? 128 : 64; }
+
 // A workgroup's tile: G lanes a row and Q groups of R rows each.  G_ = 0: G is an argument.
 template <int DT, int G_, int R_>
 struct ScanShape {
     static constexpr int N = Piece<DT>::N, R = R_;
-    static constexpr int kMostGroups = 64, kMostRows = kMostGroups * R, kMostCols = G_ > 0 ? G_ * N : kBlock;
+    static constexpr int kMostGroups = most_groups(N), kMostRows = kMostGroups * R, kMostCols = G_ > 0 ? G_ * N : kBlock;
     int G, Q;
     int C;                           // columns of the workgroup, at most kBlock
     int P;                           // threads a column
@@ -609,8 +614,10 @@ __global__ __launch_bounds__(kBlock, 3) void scan_fwd_kernel(ScanArgs a, const i
     empty_sequences(a, tile, k, cb);
 }
 
+// (Three workgroups a CU, two took 1631 us instead of 1387 for 4.2 M rows of 136 bf16; 32 values of fp32 rows are 8 rows a lane and
+// take the registers of two.)
 template <int DT, int G, int R, bool PACKED>
-__global__ __launch_bounds__(kBlock, 2) void scan_bwd_kernel(ScanArgs a, const int32_t* __restrict__ tile_seq)
+__global__ __launch_bounds__(kBlock, DT == FS_F32 && !PACKED ? 2 : 3) void scan_bwd_kernel(ScanArgs a, const int32_t* __restrict__ tile_seq)
 {
     using Shape = ScanShape<DT, G, R>;
     constexpr int N = Shape::N, LPB = kPackBlock / N;
@@ -795,7 +802,7 @@ fs_status plan_scan(int64_t n, int32_t D, fs_dtype dtype, int32_t T, int32_t B, 
     a->nb = (int)pack_blocks(D);
     const int N = dtype == FS_F32 ? 4 : 8;
     a->lanes = scan_lanes(a->units, N);
-    a->groups = kBlock / a->lanes < 64 ? kBlock / a->lanes : 64;
+    a->groups = kBlock / a->lanes < most_groups(N) ? kBlock / a->lanes : most_groups(N);
     a->by_lanes = (65536 + a->lanes - 1) / a->lanes;
     a->by_columns = (65536 + a->lanes * N - 1) / (a->lanes * N);
     const int64_t rows = (int64_t)a->groups * (values / N);
