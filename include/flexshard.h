@@ -602,7 +602,7 @@ fs_status fs_seq_unpack8(
  *   dx may be dy.  The same bits on every run (no atomics).
  * fs_seq_norm_bwd_packed -- the same with x given as a checkpoint (codes, exps
  *   of fs_seq_pack8 or fs_seq_norm_fwd); mean and rstd are those of the rows
- *   themselves.
+ *   themselves.  Both ask for the same workspace.
  *   Host faults: unknown dtype; n < 0, n >= 2^31, D < 1, a row of 4 MB or more
  *   (FS_ERR_SIZE); eps not positive and finite (FS_ERR_CONFIG); NULL; alignment
  *   as above, gamma and beta 16-byte aligned too; workspace as everywhere.
