@@ -95,6 +95,10 @@ __device__ __forceinline__ float row_sum(float v, float* lds)
     else return block_sum(v, lds);
 }
 
+// 1 / sqrt(v + eps); a variance that roundings have taken below zero counts as zero, one that is a NaN stays one (the larger of
+// it and zero would be zero).
+__device__ __forceinline__ float inverse_deviation(float var, float eps) { return 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps); }
+
 // A group of G lanes takes U rows, all their loads in flight at once.
 template <int DT, int G, int P, int U, bool PACK>
 __global__ __launch_bounds__(kBlock) void norm_fwd_kernel(NormArgs a)
@@ -151,7 +155,7 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_kernel(NormArgs a)
         }
         const float off = row_sum<G>(s1, lds) * a.inv_D;
         const float var = fmaf(-off, off, row_sum<G>(s2, lds) * a.inv_D);
-        const float rstd = 1.0f / sqrtf(fmaxf(var, 0.0f) + a.eps);
+        const float rstd = inverse_deviation(var, a.eps);
         mean += off;
         if (row >= a.n) continue;
 #pragma unroll
@@ -199,7 +203,7 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_wide_kernel(NormArgs a)
     }
     const float off = block_sum(s1, lds) * a.inv_D;
     const float var = fmaf(-off, off, block_sum(s2, lds) * a.inv_D);
-    const float rstd = 1.0f / sqrtf(fmaxf(var, 0.0f) + a.eps);
+    const float rstd = inverse_deviation(var, a.eps);
     for (int piece = threadIdx.x; piece < a.units; piece += kBlock) {
         float c[N], gamma[N], beta[N];
         Piece<DT>::unpack(x[piece], c);
