@@ -95,6 +95,9 @@ __device__ __forceinline__ float row_sum(float v, float* lds)
     else return block_sum(v, lds);
 }
 
+// The mean with what it is off.  An infinite mean (of a row with an infinity) stays: what it is off would be a NaN.
+__device__ __forceinline__ float corrected_mean(float mean, float off) { return __builtin_isinf(mean) ? mean : mean + off; }
+
 // 1 / sqrt(v + eps); a variance that roundings have taken below zero counts as zero, one that is a NaN stays one (the larger of
 // it and zero would be zero).
 __device__ __forceinline__ float inverse_deviation(float var, float eps) { return 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps); }
@@ -156,7 +159,6 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_kernel(NormArgs a)
         const float off = row_sum<G>(s1, lds) * a.inv_D;
         const float var = fmaf(-off, off, row_sum<G>(s2, lds) * a.inv_D);
         const float rstd = inverse_deviation(var, a.eps);
-        mean += off;
         if (row >= a.n) continue;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
@@ -166,7 +168,7 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_kernel(NormArgs a)
             for (int i = 0; i < N; ++i) y[i] = fmaf((c[p][i] - off) * rstd, gamma[p][i], beta[p][i]);
             store_stream(a.y + row * a.units + lig + p * G, Piece<DT>::pack(y));
         }
-        if (lig == 0 && a.mean != nullptr) { a.mean[row] = mean; a.rstd[row] = rstd; }
+        if (lig == 0 && a.mean != nullptr) { a.mean[row] = corrected_mean(mean, off); a.rstd[row] = rstd; }
     }
 }
 
@@ -213,7 +215,7 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_wide_kernel(NormArgs a)
         for (int i = 0; i < N; ++i) c[i] = fmaf((c[i] - mean - off) * rstd, gamma[i], beta[i]);
         store_stream(a.y + row * a.units + piece, Piece<DT>::pack(c));
     }
-    if (threadIdx.x == 0 && a.mean != nullptr) { a.mean[row] = mean + off; a.rstd[row] = rstd; }
+    if (threadIdx.x == 0 && a.mean != nullptr) { a.mean[row] = corrected_mean(mean, off); a.rstd[row] = rstd; }
 }
 
 // A piece of x for the backward pass, from the rows or from their checkpoint.

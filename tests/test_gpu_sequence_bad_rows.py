@@ -41,3 +41,16 @@ def test_rstd_of_a_bad_row_is_nan(dtype, units, keep):
     bad[list(BAD)] = True
     assert rstd[bad].isnan().all()
     assert same_bits(rstd[~bad], clean_rstd[~bad]) and same_bits(mean[~bad], clean_mean[~bad]) and rstd[~bad].isfinite().all()
+
+
+@pytest.mark.parametrize("keep", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("units", UNITS)
+def test_mean_of_a_row_with_an_infinity(dtype, units, keep):
+    """The sum of a row with infinities of one sign is that infinity; with both, or a NaN, it is a NaN."""
+    x, mean, *_ = statistics(dtype, units, keep)
+    with np.errstate(invalid="ignore"):
+        want = host(x).sum(1)[list(BAD)]
+    assert np.isnan(want).any() and np.isposinf(want).any() and np.isneginf(want).any()
+    got = host(mean)[list(BAD)]
+    assert np.array_equal(got, want, equal_nan=True)
