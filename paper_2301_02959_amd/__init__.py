@@ -514,6 +514,18 @@ def fs_seq_grad_bwd_update(grad_out, sorted_rows, sorted_pos, m: int, R: int, we
     return _check("fs_seq_grad_bwd_update", call(_ptr(workspace), ctypes.byref(size)), raise_on_error)
 
 
+def _int32(v: int) -> int:
+    """v for a 32-bit argument of the C call, which would get its low bits alone: one that does not fit becomes 0, a size that
+    every entry point with such an argument refuses."""
+    return v if -(1 << 31) <= v < 1 << 31 else 0
+
+
+def _tables(T: int, B: int) -> Tuple[int, int, int]:
+    """T and B for the C call, and the number of sequences: where that does not fit an int32, neither may T or B."""
+    S = T * B
+    return (T, B, S) if 0 <= S < 1 << 31 else (0, 0, S)
+
+
 def _rows(fn: str, kinds: str, rows: torch.Tensor, *tensors, sequences: int = 0) -> tuple:
     """(n, D, dtype, pointer of `rows`, pointers of the tensors that go with it ...), once those are found to be of its sizes and
     on its device, which has to be the current one (the stream is).  The library takes sizes from the caller, so a tensor that is
@@ -543,7 +555,7 @@ def _rows_checked(fn: str, kinds: str, rows: torch.Tensor, tensors: tuple, seque
         shape, dtype = wanted[kind]
         if t is not None and (tuple(t.shape) != shape or t.dtype != dtype or t.get_device() != where):
             raise ValueError(f"{fn}: expected {dtype} of shape {shape} on the device of the rows, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    return (n, D, _DTYPES[rows.dtype], _ptr(rows), *[_ptr(t) for t in tensors])
+    return (n, _int32(D), _DTYPES[rows.dtype], _ptr(rows), *[_ptr(t) for t in tensors])
 
 
 def _native_fit():
@@ -603,22 +615,24 @@ def fs_seq_norm_bwd_packed(dy, codes, exps, mean, rstd, gamma, dx, dgamma, dbeta
 def seq_norm_bwd_workspace_bytes(n: int, D: int, dtype: int) -> int:
     """The packed form needs the same."""
     size = ctypes.c_size_t(0)
-    code = _typed().fs_seq_norm_bwd(None, None, None, None, n, D, dtype, None, None, None, None, None, ctypes.byref(size), None)
+    code = _typed().fs_seq_norm_bwd(None, None, None, None, n, _int32(D), dtype, None, None, None, None, None, ctypes.byref(size), None)
     _check("fs_seq_norm_bwd", code, True)
     return int(size.value)
 
 
 def fs_seq_scan_fwd(x, gate, offsets, T: int, B: int, h0, h, h_last=None, dev_status=None,
                     workspace: Optional[torch.Tensor] = None, raise_on_error: bool = True) -> int:
-    n, D, dtype, x_, gate_, offsets_, h0_, h_, last_ = _rows("fs_seq_scan_fwd", "sotst", x, gate, offsets, h0, h, h_last, sequences=T * B)
+    T, B, S = _tables(T, B)
+    n, D, dtype, x_, gate_, offsets_, h0_, h_, last_ = _rows("fs_seq_scan_fwd", "sotst", x, gate, offsets, h0, h, h_last, sequences=S)
     return _with_workspace("fs_seq_scan_fwd", _typed().fs_seq_scan_fwd, (x_, gate_, n, D, dtype, offsets_, T, B, h0_, h_, last_),
                            (_stream(), _ptr(dev_status, _I32)), x.device, workspace, raise_on_error)
 
 
 def fs_seq_scan_bwd(dh, dh_last, x, gate, h, offsets, T: int, B: int, h0, dx, dgate, dh0=None, dev_status=None,
                     workspace: Optional[torch.Tensor] = None, raise_on_error: bool = True) -> int:
+    T, B, S = _tables(T, B)
     n, D, dtype, dh_, last_, x_, gate_, h_, offsets_, *rest = _rows("fs_seq_scan_bwd", "tsssotsst", dh, dh_last, x, gate, h, offsets, h0, dx, dgate,
-                                                                    dh0, sequences=T * B)
+                                                                    dh0, sequences=S)
     return _with_workspace("fs_seq_scan_bwd", _typed().fs_seq_scan_bwd, (dh_, last_, x_, gate_, h_, n, D, dtype, offsets_, T, B, *rest),
                            (_stream(), _ptr(dev_status, _I32)), dh.device, workspace, raise_on_error)
 
@@ -626,15 +640,16 @@ def fs_seq_scan_bwd(dh, dh_last, x, gate, h, offsets, T: int, B: int, h0, dx, dg
 def fs_seq_scan_bwd_packed(dh, dh_last, x_codes, x_exps, gate_codes, gate_exps, h_codes, h_exps, offsets, T: int, B: int,
                            h0, dx, dgate, dh0=None, dev_status=None, workspace: Optional[torch.Tensor] = None,
                            raise_on_error: bool = True) -> int:
+    T, B, S = _tables(T, B)
     n, D, dtype, *got = _rows("fs_seq_scan_bwd_packed", "tpepepeotsst", dh, dh_last, x_codes, x_exps, gate_codes, gate_exps, h_codes, h_exps,
-                              offsets, h0, dx, dgate, dh0, sequences=T * B)
+                              offsets, h0, dx, dgate, dh0, sequences=S)
     return _with_workspace("fs_seq_scan_bwd_packed", _typed().fs_seq_scan_bwd_packed, (*got[:8], n, D, dtype, got[8], T, B, *got[9:]),
                            (_stream(), _ptr(dev_status, _I32)), dh.device, workspace, raise_on_error)
 
 
 def seq_scan_fwd_workspace_bytes(n: int, D: int, dtype: int, T: int, B: int) -> int:
     size = ctypes.c_size_t(0)
-    code = _typed().fs_seq_scan_fwd(None, None, n, D, dtype, None, T, B, None, None, None, None, ctypes.byref(size), None, None)
+    code = _typed().fs_seq_scan_fwd(None, None, n, _int32(D), dtype, None, *_tables(T, B)[:2], None, None, None, None, ctypes.byref(size), None, None)
     _check("fs_seq_scan_fwd", code, True)
     return int(size.value)
 
@@ -642,7 +657,7 @@ def seq_scan_fwd_workspace_bytes(n: int, D: int, dtype: int, T: int, B: int) -> 
 def seq_scan_bwd_workspace_bytes(n: int, D: int, dtype: int, T: int, B: int) -> int:
     """The packed form needs the same."""
     size = ctypes.c_size_t(0)
-    code = _typed().fs_seq_scan_bwd(None, None, None, None, None, n, D, dtype, None, T, B, None, None, None, None, None,
+    code = _typed().fs_seq_scan_bwd(None, None, None, None, None, n, _int32(D), dtype, None, *_tables(T, B)[:2], None, None, None, None, None,
                                     ctypes.byref(size), None, None)
     _check("fs_seq_scan_bwd", code, True)
     return int(size.value)

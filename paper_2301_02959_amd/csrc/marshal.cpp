@@ -83,6 +83,7 @@ static PyObject* rows_that_fit(PyObject*, PyObject* const* args, Py_ssize_t narg
         const int code = type == at::kFloat ? 0 : type == at::kHalf ? 1 : type == at::kBFloat16 ? 2 : -1;
         if (code < 0 || !rows.is_cuda() || rows.dim() != 2) Py_RETURN_NONE;
         const int64_t n = rows.size(0), D = rows.size(1);
+        if (D > INT32_MAX) Py_RETURN_NONE;        // the C call's D has 32 bits
         out = PyTuple_New(4 + count);
         if (out == nullptr) return nullptr;
         PyTuple_SET_ITEM(out, 0, PyLong_FromLongLong(n));

@@ -1,0 +1,87 @@
+"""Sizes that do not fit the C entry points' 32-bit integers: the binding refuses them instead of handing on their low bits.  No
+GPU: tensors without elements, whose pointers nothing reads."""
+import ctypes
+import os
+
+import pytest
+import torch
+
+import paper_2301_02959_amd as fs
+
+pytestmark = pytest.mark.skipif(not os.path.exists(fs.LIB_PATH), reason="library not built (run __graft_entry__.build())")
+
+SIZE = 2
+WIDE = [1 << 31, (1 << 32) + 8, (1 << 33) + 64]         # as an int32: negative, 8, 64
+
+
+@pytest.fixture(autouse=True)
+def host_pointers(monkeypatch):
+    monkeypatch.setattr(fs, "_ptr", lambda t, dtypes=None: None if t is None else t.data_ptr())
+    monkeypatch.setattr(fs, "_stream", lambda: None)
+
+
+def refused(call, *args, **more):
+    assert call(*args, raise_on_error=False, **more) == SIZE
+    with pytest.raises(fs.FlexShardError):
+        call(*args, **more)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("D", WIDE)
+def test_rows_of_more_columns_than_an_int32_counts(D, dtype):
+    """No rows, so nothing is allocated and nothing would be written; before rows are counted, D is refused."""
+    x = torch.empty(0, D, dtype=dtype)
+    f = torch.empty(0, D)
+    codes, exps = torch.empty(0, D, dtype=torch.int8), torch.empty(0, -(-D // 32), dtype=torch.uint8)
+    ws = torch.empty(256, dtype=torch.uint8)
+    off, none = torch.zeros(2, dtype=torch.int64), torch.empty(0)
+    refused(fs.fs_seq_pack8, x, codes, exps)
+    refused(fs.fs_seq_unpack8, codes, exps, x)
+    refused(fs.fs_seq_scan_step, x, x, f, f, x)
+    refused(fs.fs_seq_norm_fwd, x, None, None, 1e-5, x)
+    for more in ({}, {"workspace": ws}):
+        refused(fs.fs_seq_norm_bwd, x, x, none, none, None, x, None, None, **more)
+        refused(fs.fs_seq_norm_bwd_packed, x, codes, exps, none, none, None, x, None, None, **more)
+        refused(fs.fs_seq_scan_fwd, x, x, off, 1, 1, None, x, **more)
+        refused(fs.fs_seq_scan_bwd, x, None, x, x, x, off, 1, 1, None, x, x, **more)
+        refused(fs.fs_seq_scan_bwd_packed, x, None, codes, exps, codes, exps, codes, exps, off, 1, 1, None, x, x, **more)
+
+
+@pytest.mark.parametrize("big", WIDE + [(1 << 32) + 1])
+def test_workspaces_of_sizes_past_an_int32(big):
+    for size in (lambda: fs.seq_norm_bwd_workspace_bytes(5, big, 0), lambda: fs.seq_scan_fwd_workspace_bytes(5, big, 0, 1, 1),
+                 lambda: fs.seq_scan_bwd_workspace_bytes(5, big, 0, 1, 1), lambda: fs.seq_scan_fwd_workspace_bytes(5, 64, 0, big, 1),
+                 lambda: fs.seq_scan_fwd_workspace_bytes(5, 64, 0, 1, big), lambda: fs.seq_scan_bwd_workspace_bytes(5, 64, 0, big, 1),
+                 lambda: fs.seq_scan_bwd_workspace_bytes(5, 64, 0, 1, big)):
+        with pytest.raises(fs.FlexShardError) as e:
+            size()
+        assert e.value.code == SIZE
+
+
+class Offsets(torch.Tensor):
+    """Stands for the offsets of more sequences than this machine has memory for."""
+    @staticmethod
+    def __new__(cls, count):
+        t = torch.Tensor._make_subclass(cls, torch.zeros(2, dtype=torch.int64))
+        t.count = count
+        return t
+
+    shape = property(lambda self: torch.Size([self.count]))
+
+
+@pytest.mark.parametrize("T, B", [((1 << 32) + 1, 1), (1, (1 << 32) + 1), (1 << 31, 1), (1 << 16, 1 << 15), ((1 << 32) + 2, 3)])
+def test_more_sequences_than_an_int32_counts(T, B):
+    x = torch.empty(0, 64)
+    codes, exps = torch.empty(0, 64, dtype=torch.int8), torch.empty(0, 2, dtype=torch.uint8)
+    off = Offsets(T * B + 1)
+    ws = torch.empty(1 << 20, dtype=torch.uint8)
+    for more in ({}, {"workspace": ws}):
+        refused(fs.fs_seq_scan_fwd, x, x, off, T, B, None, x, **more)
+        refused(fs.fs_seq_scan_bwd, x, None, x, x, x, off, T, B, None, x, x, **more)
+        refused(fs.fs_seq_scan_bwd_packed, x, None, codes, exps, codes, exps, codes, exps, off, T, B, None, x, x, **more)
+
+
+def test_the_c_calls_refuse_what_the_binding_hands_them():
+    asked = ctypes.c_size_t(0)
+    assert fs._typed().fs_seq_pack8(None, 0, 0, 0, None, None, None) == SIZE
+    assert fs._typed().fs_seq_scan_fwd(None, None, 0, 64, 0, None, 0, 1, None, None, None, None, ctypes.byref(asked), None, None) == SIZE
