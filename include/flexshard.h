@@ -660,7 +660,8 @@ fs_status fs_seq_norm_bwd_packed(
  * that a workgroup has at a time, less than 4 % of x forward and 8 % backward;
  * nothing in it has to survive from call to call or start at any value.
  * Host faults: unknown dtype; n < 0, n >= 2^31, D < 1, T < 1, B < 1,
- * T*B >= 2^31, a row of 4 MB or more, over 64 GB in x (FS_ERR_SIZE); NULL;
+ * T*B >= 2^31, a row of 4 MB or more, more than 2^24 - 1 stretches of rows and
+ * columns (over 240 GB in x), for the step over 64 GB in x (FS_ERR_SIZE); NULL;
  * alignment as above, h0, h_last, dh_last, dh0 and the states 16-byte aligned
  * too; workspace as everywhere.
  */

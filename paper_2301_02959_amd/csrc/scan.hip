@@ -808,9 +808,11 @@ fs_status plan_scan(int64_t n, int32_t D, fs_dtype dtype, int32_t T, int32_t B, 
     const int64_t rows = (int64_t)a->groups * (values / N);
     a->col_blocks = (a->units + a->lanes - 1) / a->lanes;
     a->tiles = (n + rows - 1) / rows;
-    const int64_t passes = (a->S + kBlock - 1) / kBlock;            // workgroups that the sequences alone would keep busy
-    a->strides = a->tiles > passes ? a->tiles : passes < 1024 ? passes : a->tiles > 1024 ? a->tiles : 1024;
-    if (a->strides * a->col_blocks > kMostGrid) return FS_ERR_SIZE;         // (over 64 GB a tensor)
+    if (a->tiles * a->col_blocks > kMostGrid) return FS_ERR_SIZE;   // (over 240 GB in x: 14400 bytes of it a workgroup or more)
+    // where the tiles are few, more workgroups share the sequences' passes of 256: up to 1024 of them, as many as a launch has room for
+    const int64_t passes = (a->S + kBlock - 1) / kBlock, room = kMostGrid / a->col_blocks;
+    const int64_t most = room < 1024 ? room : 1024, shared = passes < most ? passes : most;
+    a->strides = a->tiles > shared ? a->tiles : shared;
     uint32_t* const ticket = ws->take<uint32_t>(1);                 // always: a workspace of no bytes could be null, which is a question
     if (a->tiles > 1) {
         a->words = ws->take<uint64_t>((size_t)(a->tiles + a->tiles / kSpan) * (size_t)a->col_blocks * (size_t)(a->lanes * N));

@@ -21,3 +21,26 @@ def test_more_columns_than_an_int32_counts(D):
         assert e.value.code == 2
     narrow = torch.empty(0, (1 << 31) - 8, dtype=torch.float16, device=DEV)
     assert fs._fit("", 0, 0, narrow)[:3] == (0, (1 << 31) - 8, fs.FS_F16)
+
+
+@pytest.mark.parametrize("S", [3, 1 << 18, 3_000_001])
+def test_wide_rows_in_many_sequences(S):
+    """Three rows of just under 4 MB, and many sequences without rows behind theirs: the same bits however many those are."""
+    D = ((1 << 18) - 8) * 8
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    x, gate, dh = (torch.randn(3, D, generator=gen, device=DEV).bfloat16() for _ in range(3))
+    got = []
+    for count in (3, S):
+        off = torch.full((count + 1,), 3, device=DEV)
+        off[:3] = torch.tensor([0, 1, 1])
+        st = torch.zeros(1, dtype=torch.int32, device=DEV)
+        h, dx, dg = (torch.full_like(x, 7.0) for _ in range(3))
+        fs.fs_seq_scan_fwd(x, gate, off, 1, count, None, h, None, st)
+        fs.fs_seq_scan_bwd(dh, None, x, gate, h, off, 1, count, None, dx, dg, None, st)
+        assert int(st.item()) == 0
+        off[-1] = 4                                          # the sequences' last bound is looked at too
+        fs.fs_seq_scan_fwd(x, gate, off, 1, count, None, torch.empty_like(h), None, st)
+        assert int(st.item()) == fs.FS_DEV_BAD_OFFSETS
+        got.append((h, dx, dg))
+    for a, b in zip(*got):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))

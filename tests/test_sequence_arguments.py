@@ -85,3 +85,37 @@ def test_the_c_calls_refuse_what_the_binding_hands_them():
     asked = ctypes.c_size_t(0)
     assert fs._typed().fs_seq_pack8(None, 0, 0, 0, None, None, None) == SIZE
     assert fs._typed().fs_seq_scan_fwd(None, None, 0, 64, 0, None, 0, 1, None, None, None, None, ctypes.byref(asked), None, None) == SIZE
+
+
+def asked_for(name, n, D, dtype, S):
+    """(status, bytes) of the recurrence's question for its workspace."""
+    asked = ctypes.c_size_t(0)
+    pointers = {"fs_seq_scan_fwd": ((None,) * 2, (None,) * 3), "fs_seq_scan_bwd": ((None,) * 5, (None,) * 4), "fs_seq_scan_bwd_packed": ((None,) * 8, (None,) * 4)}
+    front, behind = pointers[name]
+    code = getattr(fs._typed(), name)(*front, n, D, dtype, None, 1, S, *behind, None, ctypes.byref(asked), None, None)
+    return code, asked.value
+
+
+SCANS = ["fs_seq_scan_fwd", "fs_seq_scan_bwd", "fs_seq_scan_bwd_packed"]
+
+
+@pytest.mark.parametrize("name", SCANS)
+def test_wide_rows_in_many_sequences(name):
+    """Few rows of many columns among more sequences than rows: the size of x decides, not the sequences times the columns."""
+    for dtype, N in ((0, 4), (1, 8), (2, 8)):
+        for units in ((1 << 18) - 1, (1 << 18) - 8, (1 << 17) + 8, 5000, 1):
+            D = units * N
+            for S in (1, 1 << 17, 1 << 18, 1 << 24, (1 << 31) - 1):
+                for n in (0, 1, 5, 3000):
+                    assert asked_for(name, n, D, dtype, S)[0] == 0, (n, D, dtype, S)
+
+
+@pytest.mark.parametrize("name", SCANS)
+def test_batches_too_large_for_one_launch(name):
+    """2^24 workgroups of 256 threads are more than a launch takes.  No width reaches them below 200 GB in x."""
+    for dtype, N in ((0, 4), (1, 8)):
+        for units in (1, 2, 3, 9, 16, 17, 29, 31, 33, 65, 127, 1000, 4097, 99999, (1 << 18) - 1):
+            n = min((1 << 31) - 1, 200 * 10 ** 9 // (16 * units))
+            assert asked_for(name, n, units * N, dtype, 7)[0] == 0, (dtype, units)
+        n = (1 << 31) - 1
+        assert asked_for(name, n, 4096 * N, dtype, 7)[0] == SIZE and asked_for(name, n, ((1 << 18) - 1) * N, dtype, 7)[0] == SIZE
