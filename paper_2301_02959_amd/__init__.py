@@ -586,6 +586,14 @@ def fs_seq_norm_fwd(x, gamma, beta, eps: float, y, mean=None, rstd=None, codes=N
     return _check("fs_seq_norm_fwd", code, raise_on_error)
 
 
+def _ptr_here(fn: str, t: Optional[torch.Tensor], dtypes: Optional[tuple] = None) -> Optional[int]:
+    """_ptr of a workspace or a status word, which has to be on the current device as _rows finds the operands to be."""
+    pointer = _ptr(t, dtypes)
+    if t is not None and t.get_device() != _raw_device():
+        raise ValueError(f"{fn}: got a tensor on {t.device}, the current device is {_raw_device()}")
+    return pointer
+
+
 def _with_workspace(fn: str, entry, args: tuple, tail: tuple, device, workspace: Optional[torch.Tensor], raise_on_error: bool) -> int:
     """entry(*args, workspace, its size, *tail) with the caller's workspace, or one of the size that the entry point asks for."""
     if workspace is None:
@@ -594,7 +602,7 @@ def _with_workspace(fn: str, entry, args: tuple, tail: tuple, device, workspace:
             return _check(fn, code, raise_on_error)
     else:
         size = ctypes.c_size_t(workspace.numel() * workspace.element_size())
-    return _check(fn, entry(*args, _ptr(workspace), ctypes.byref(size), *tail), raise_on_error)
+    return _check(fn, entry(*args, _ptr_here(fn, workspace), ctypes.byref(size), *tail), raise_on_error)
 
 
 def fs_seq_norm_bwd(dy, x, mean, rstd, gamma, dx, dgamma, dbeta, workspace: Optional[torch.Tensor] = None,
@@ -625,7 +633,7 @@ def fs_seq_scan_fwd(x, gate, offsets, T: int, B: int, h0, h, h_last=None, dev_st
     T, B, S = _tables(T, B)
     n, D, dtype, x_, gate_, offsets_, h0_, h_, last_ = _rows("fs_seq_scan_fwd", "sotst", x, gate, offsets, h0, h, h_last, sequences=S)
     return _with_workspace("fs_seq_scan_fwd", _typed().fs_seq_scan_fwd, (x_, gate_, n, D, dtype, offsets_, T, B, h0_, h_, last_),
-                           (_stream(), _ptr(dev_status, _I32)), x.device, workspace, raise_on_error)
+                           (_stream(), _ptr_here("fs_seq_scan_fwd", dev_status, _I32)), x.device, workspace, raise_on_error)
 
 
 def fs_seq_scan_bwd(dh, dh_last, x, gate, h, offsets, T: int, B: int, h0, dx, dgate, dh0=None, dev_status=None,
@@ -634,7 +642,7 @@ def fs_seq_scan_bwd(dh, dh_last, x, gate, h, offsets, T: int, B: int, h0, dx, dg
     n, D, dtype, dh_, last_, x_, gate_, h_, offsets_, *rest = _rows("fs_seq_scan_bwd", "tsssotsst", dh, dh_last, x, gate, h, offsets, h0, dx, dgate,
                                                                     dh0, sequences=S)
     return _with_workspace("fs_seq_scan_bwd", _typed().fs_seq_scan_bwd, (dh_, last_, x_, gate_, h_, n, D, dtype, offsets_, T, B, *rest),
-                           (_stream(), _ptr(dev_status, _I32)), dh.device, workspace, raise_on_error)
+                           (_stream(), _ptr_here("fs_seq_scan_bwd", dev_status, _I32)), dh.device, workspace, raise_on_error)
 
 
 def fs_seq_scan_bwd_packed(dh, dh_last, x_codes, x_exps, gate_codes, gate_exps, h_codes, h_exps, offsets, T: int, B: int,
@@ -644,7 +652,7 @@ def fs_seq_scan_bwd_packed(dh, dh_last, x_codes, x_exps, gate_codes, gate_exps, 
     n, D, dtype, *got = _rows("fs_seq_scan_bwd_packed", "tpepepeotsst", dh, dh_last, x_codes, x_exps, gate_codes, gate_exps, h_codes, h_exps,
                               offsets, h0, dx, dgate, dh0, sequences=S)
     return _with_workspace("fs_seq_scan_bwd_packed", _typed().fs_seq_scan_bwd_packed, (*got[:8], n, D, dtype, got[8], T, B, *got[9:]),
-                           (_stream(), _ptr(dev_status, _I32)), dh.device, workspace, raise_on_error)
+                           (_stream(), _ptr_here("fs_seq_scan_bwd_packed", dev_status, _I32)), dh.device, workspace, raise_on_error)
 
 
 def seq_scan_fwd_workspace_bytes(n: int, D: int, dtype: int, T: int, B: int) -> int:

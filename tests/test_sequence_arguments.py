@@ -18,6 +18,7 @@ WIDE = [1 << 31, (1 << 32) + 8, (1 << 33) + 64]         # as an int32: negative,
 def host_pointers(monkeypatch):
     monkeypatch.setattr(fs, "_ptr", lambda t, dtypes=None: None if t is None else t.data_ptr())
     monkeypatch.setattr(fs, "_stream", lambda: None)
+    monkeypatch.setattr(fs, "_raw_device", lambda: -1)       # what host tensors call their device
 
 
 def refused(call, *args, **more):
@@ -119,3 +120,32 @@ def test_batches_too_large_for_one_launch(name):
             assert asked_for(name, n, units * N, dtype, 7)[0] == 0, (dtype, units)
         n = (1 << 31) - 1
         assert asked_for(name, n, 4096 * N, dtype, 7)[0] == SIZE and asked_for(name, n, ((1 << 18) - 1) * N, dtype, 7)[0] == SIZE
+
+
+class Elsewhere(torch.Tensor):
+    """A tensor of another device than the rows."""
+    @staticmethod
+    def __new__(cls, t):
+        return torch.Tensor._make_subclass(cls, t)
+
+    def get_device(self):
+        return 1
+
+
+def test_workspaces_and_status_words_of_another_device():
+    """The kernels run on the current device; they would read and write the other one's memory."""
+    x, off = torch.empty(0, 64), torch.zeros(2, dtype=torch.int64)
+    codes, exps, none = torch.empty(0, 64, dtype=torch.int8), torch.empty(0, 2, dtype=torch.uint8), torch.empty(0)
+    ws, st = torch.empty(1 << 16, dtype=torch.uint8), torch.zeros(1, dtype=torch.int32)
+    scans = [lambda **more: fs.fs_seq_scan_fwd(x, x, off, 1, 1, None, x, **more),
+             lambda **more: fs.fs_seq_scan_bwd(x, None, x, x, x, off, 1, 1, None, x, x, **more),
+             lambda **more: fs.fs_seq_scan_bwd_packed(x, None, codes, exps, codes, exps, codes, exps, off, 1, 1, None, x, x, **more)]
+    norms = [lambda **more: fs.fs_seq_norm_bwd(x, x, none, none, None, x, None, None, **more),
+             lambda **more: fs.fs_seq_norm_bwd_packed(x, codes, exps, none, none, None, x, None, None, **more)]
+    for call in scans + norms:
+        with pytest.raises(ValueError):
+            call(workspace=Elsewhere(ws))
+    for call in scans:
+        for more in ({}, {"workspace": ws}):
+            with pytest.raises(ValueError):
+                call(dev_status=Elsewhere(st), **more)
