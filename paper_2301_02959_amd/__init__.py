@@ -28,6 +28,7 @@ FS_TIER_CUTS = 10
 FS_MAX_BUCKETS = 4096
 FS_ROUTE_NOALLOC_SCRATCH_BYTES = 32 << 20
 
+FS_ERR_WORKSPACE = 5
 STATUS_NAMES = {0: "FS_OK", 1: "FS_ERR_NULL", 2: "FS_ERR_SIZE", 3: "FS_ERR_DTYPE", 4: "FS_ERR_ALIGN",
                 5: "FS_ERR_WORKSPACE", 6: "FS_ERR_CONFIG", 7: "FS_ERR_DEVICE"}
 
@@ -602,7 +603,10 @@ def _with_workspace(fn: str, entry, args: tuple, tail: tuple, device, workspace:
             return _check(fn, code, raise_on_error)
     else:
         size = ctypes.c_size_t(workspace.numel() * workspace.element_size())
-    return _check(fn, entry(*args, _ptr_here(fn, workspace), ctypes.byref(size), *tail), raise_on_error)
+    pointer = _ptr_here(fn, workspace)
+    if not pointer:                              # a workspace of no bytes: the library would take it for the question
+        return _check(fn, FS_ERR_WORKSPACE, raise_on_error)
+    return _check(fn, entry(*args, pointer, ctypes.byref(size), *tail), raise_on_error)
 
 
 def fs_seq_norm_bwd(dy, x, mean, rstd, gamma, dx, dgamma, dbeta, workspace: Optional[torch.Tensor] = None,

@@ -149,3 +149,19 @@ def test_workspaces_and_status_words_of_another_device():
         for more in ({}, {"workspace": ws}):
             with pytest.raises(ValueError):
                 call(dev_status=Elsewhere(st), **more)
+
+
+def test_a_workspace_without_bytes_is_too_small():
+    """It has no address, and a call without one asks for the size instead of running."""
+    x, off = torch.empty(0, 64), torch.zeros(2, dtype=torch.int64)
+    codes, exps, none = torch.empty(0, 64, dtype=torch.int8), torch.empty(0, 2, dtype=torch.uint8), torch.empty(0)
+    nothing = torch.empty(0, dtype=torch.uint8)
+    assert nothing.data_ptr() == 0
+    for call in (lambda **more: fs.fs_seq_scan_fwd(x, x, off, 1, 1, None, x, workspace=nothing, **more),
+                 lambda **more: fs.fs_seq_scan_bwd(x, None, x, x, x, off, 1, 1, None, x, x, workspace=nothing, **more),
+                 lambda **more: fs.fs_seq_scan_bwd_packed(x, None, codes, exps, codes, exps, codes, exps, off, 1, 1, None, x, x, workspace=nothing, **more),
+                 lambda **more: fs.fs_seq_norm_bwd(x, x, none, none, None, x, None, None, workspace=nothing, **more),
+                 lambda **more: fs.fs_seq_norm_bwd_packed(x, codes, exps, none, none, None, x, None, None, workspace=nothing, **more)):
+        assert call(raise_on_error=False) == 5
+        with pytest.raises(fs.FlexShardError):
+            call()
