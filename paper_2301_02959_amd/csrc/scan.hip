@@ -25,6 +25,7 @@
 #include <type_traits>
 
 #include "pack8.h"
+#include "seq_marks.h"
 #include "seq_rows.h"
 
 namespace fs {
@@ -54,7 +55,7 @@ struct ScanArgs {
     int lanes, groups;               // of a workgroup
     int by_lanes, by_columns;        // t / lanes and t / (columns of a workgroup) as (t * this) >> 16, t <= kBlock
     uint64_t* words;                 // [tiles + spans of kSpan tiles][col_blocks][columns of a workgroup]
-    int32_t* tile_seq;               // [tiles]: the sequence that the row before the tile is in
+    int32_t* tile_seq;               // [tiles + 1]: the sequence that the row before the tile is in
     uint32_t* ticket;                // null: one tile, nothing to wait for
 };
 
@@ -187,50 +188,74 @@ struct ScanShared {
     uint32_t ticket;
 };
 
-// The bounds of the 64 sequences from the one on that the row before the tile is in, one a lane of the first wave.  Loaded in
+// The bounds of the 64 sequences from the one on that the row before the tile is in, one a lane of every wave.  Loaded in
 // front of the rows: loads come back in their order, and behind the rows the marks would wait for all of them.
 struct Bounds {
     int64_t s, b, e;
-    __device__ __forceinline__ void load(const ScanArgs& a)
-    {
-        b = e = a.n;
-        if (s < a.S) { b = a.offsets[s]; e = a.offsets[s + 1]; }
-    }
     __device__ __forceinline__ Bounds(const ScanArgs& a, int s0)
     {
         s = (int64_t)(s0 < 0 ? 0 : s0) + lane_id();     // (s0 is at most S - 1)
-        load(a);
+        b = e = a.n;
+        if (s < a.S) { b = a.offsets[s]; e = a.offsets[s + 1]; }
     }
 };
 
-// Marks the first and last rows of the sequences in the tile from row0 on; the first wave does it.  With bad offsets the marks
-// are arbitrary but inside the tile.
 template <class Shape>
-__device__ __forceinline__ void mark_sequences(const ScanArgs& a, const Shape& tile, int64_t row0, Bounds seqs, ScanShared<Shape>* sh)
+__device__ __forceinline__ void mark_first(ScanShared<Shape>* sh, int row, int32_t s)
 {
-    const int lane = lane_id();
-    if (lane < Shape::kMostRows / 32) sh->firsts[lane] = sh->lasts[lane] = 0u;
+    atomicOr(&sh->firsts[row >> 5], 1u << (row & 31));
+    sh->first_of[row] = s;
+}
+
+template <class Shape>
+__device__ __forceinline__ void mark_last(ScanShared<Shape>* sh, int row, int32_t s)
+{
+    atomicOr(&sh->lasts[row >> 5], 1u << (row & 31));
+    sh->last_of[row] = s;
+}
+
+// Sequence s with rows b .. e - 1, of a tile of `rows` rows from row0 on.
+template <class Shape>
+__device__ __forceinline__ void mark_sequence(ScanShared<Shape>* sh, int64_t row0, int rows, int64_t s, int64_t b, int64_t e)
+{
+    if (b >= e) return;
+    b -= row0;
+    e -= row0;
+    if (b >= 0 && b < rows) mark_first(sh, (int)b, (int32_t)s);
+    if (e > 0 && e <= rows) mark_last(sh, (int)e - 1, (int32_t)s);
+}
+
+// Marks the first and last rows of the sequences in tile `number`, from row0 on; every thread calls it.  The first wave takes
+// the 64 sequences of `mine`, which mostly is all; where there are more, all threads take the others, and where those are very
+// many, each row finds its own: what a tile takes does not grow with the sequences without rows in it.  Contains barriers.
+// With bad offsets the marks are arbitrary but inside the tile.
+template <class Shape>
+__device__ __forceinline__ void mark_sequences(const ScanArgs& a, const Shape& tile, const int32_t* tile_seq, int64_t number, int64_t row0,
+                                               const Bounds& mine, ScanShared<Shape>* sh)
+{
     const int rows = a.n - row0 < tile.T ? (int)(a.n - row0) : tile.T;
-    const auto mark = [&] {
-        const int64_t b = seqs.b - row0, e = seqs.e - row0;
-        if (b < e) {
-            if (b >= 0 && b < rows) {
-                const int at = (int)b;
-                atomicOr(&sh->firsts[at >> 5], 1u << (at & 31));
-                sh->first_of[at] = (int32_t)seqs.s;
-            }
-            if (e > 0 && e <= rows) {
-                const int at = (int)e - 1;
-                atomicOr(&sh->lasts[at >> 5], 1u << (at & 31));
-                sh->last_of[at] = (int32_t)seqs.s;
-            }
-        }
-        return (ballot(b < rows && seqs.s < a.S) >> (kWave - 1)) != 0;          // the last lane's begins in the tile or before it
-    };
-    for (bool more = mark(); more; more = mark()) {
-        seqs.s += kWave;
-        seqs.load(a);
+    if (wave_id() == 0) {
+        const int lane = lane_id();
+        if (lane < Shape::kMostRows / 32) sh->firsts[lane] = sh->lasts[lane] = 0u;
+        mark_sequence(sh, row0, rows, mine.s, mine.b, mine.e);
     }
+    const bool more = (ballot(mine.b - row0 < rows && mine.s < a.S) >> (kWave - 1)) != 0;     // the last lane's begins in the tile or before it
+    __syncthreads();
+    if (!more) return;
+    const uint32_t first = tile_seq == nullptr ? 0u : (uint32_t)tile_seq[number];
+    const uint32_t last = tile_seq == nullptr ? (uint32_t)(a.S - 1) : (uint32_t)tile_seq[number + 1];      // the last that begins in the tile
+    const uint32_t count = last < first ? 0u : last - first + 1u;                                          // (0: bad offsets)
+    if (mark_rounds(count) <= kMostMarkRounds) {
+        for (int64_t s = (int64_t)first + kWave + threadIdx.x; s <= last; s += kBlock) mark_sequence(sh, row0, rows, s, a.offsets[s], a.offsets[s + 1]);
+    } else {
+        for (int row = threadIdx.x; row < rows; row += kBlock) {
+            const int64_t at = row0 + row;
+            const uint32_t s = sequence_of_row(first, count, at, [&](uint32_t i) { return a.offsets[i]; });
+            if (a.offsets[s] == at) mark_first(sh, row, (int32_t)s);
+            if (a.offsets[s + 1] == at + 1) mark_last(sh, row, (int32_t)s);
+        }
+    }
+    __syncthreads();
 }
 
 // Marks of the thread's group, bit r for row r.
@@ -548,8 +573,7 @@ __global__ __launch_bounds__(kBlock, 3) void scan_fwd_kernel(ScanArgs a, const i
             raw_g[r] = load_rows<(G > 0)>(piece_at(from_g, p.at(r)));
             raw_x[r] = load_rows<(G > 0)>(piece_at(from_x, p.at(r)));
         }
-        if (wave_id() == 0) mark_sequences(a, tile, p.row0, bounds, &sh);
-        __syncthreads();
+        mark_sequences(a, tile, tile_seq, k, p.row0, bounds, &sh);
         const uint32_t firsts = group_marks(tile, sh.firsts);
         const uint32_t lasts = group_marks(tile, sh.lasts);
         float f[R][N], b[R][N];
@@ -647,8 +671,7 @@ __global__ __launch_bounds__(kBlock, DT == FS_F32 && !PACKED ? 2 : 3) void scan_
             const uint32_t up = p.row0 > 0 || row == 0 ? 0u : 1u;               // the batch's first row stands in for the one before it
             before[r].load(a, p.row0 > 0 ? p.row0 - 1 : 0, p.at(r) - up * p.units, block - up * (uint32_t)a.nb);
         }
-        if (wave_id() == 0) mark_sequences(a, tile, p.row0, bounds, &sh);
-        __syncthreads();
+        mark_sequences(a, tile, tile_seq, a.tiles - 1 - k, p.row0, bounds, &sh);
         const uint32_t firsts = group_marks(tile, sh.firsts), lasts = group_marks(tile, sh.lasts);
         float f[R][N], o[R][N], d[R][N];
         float A[N], B[N];
@@ -728,18 +751,19 @@ __global__ __launch_bounds__(kBlock, DT == FS_F32 && !PACKED ? 2 : 3) void scan_
 }
 
 // All words not ready, no ticket taken, and every tile's first sequence: the largest s with offsets[s] <= the row before it
-// (bad offsets: some s in [0, S)).  A thread a tile bisects here, beside the writes of the others; in the tiles' own workgroups
+// (bad offsets: some s in [0, S)); behind the last tile's the same for the batch's end.  A thread a tile bisects here, beside the writes of the others; in the tiles' own workgroups
 // the search is a chain of loads in front of everything.
 __global__ __launch_bounds__(kBlock) void scan_clear_kernel(ScanArgs a, int64_t pieces, int tile_rows)
 {
     const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
     if (i < pieces) reinterpret_cast<u32x4*>(a.words)[i] = u32x4{~0u, ~0u, ~0u, ~0u};
     if (i == 0) *a.ticket = 0u;
-    if (i >= a.tiles) return;
-    int64_t lo = 0, hi = a.S;                            // offsets[lo] <= i * tile_rows - 1 (taken as given for lo = 0) < offsets[hi]
+    if (i > a.tiles) return;
+    const int64_t row = i < a.tiles ? i * tile_rows : a.n;
+    int64_t lo = 0, hi = a.S;                            // offsets[lo] < row (taken as given for lo = 0) <= offsets[hi]
     while (hi - lo > 1) {
         const int64_t mid = lo + ((hi - lo) >> 1);
-        if (a.offsets[mid] < i * tile_rows) lo = mid; else hi = mid;
+        if (a.offsets[mid] < row) lo = mid; else hi = mid;
     }
     a.tile_seq[i] = (int32_t)lo;
 }
@@ -816,7 +840,7 @@ fs_status plan_scan(int64_t n, int32_t D, fs_dtype dtype, int32_t T, int32_t B, 
     uint32_t* const ticket = ws->take<uint32_t>(1);                 // always: a workspace of no bytes could be null, which is a question
     if (a->tiles > 1) {
         a->words = ws->take<uint64_t>((size_t)(a->tiles + a->tiles / kSpan) * (size_t)a->col_blocks * (size_t)(a->lanes * N));
-        a->tile_seq = ws->take<int32_t>((size_t)a->tiles);
+        a->tile_seq = ws->take<int32_t>((size_t)a->tiles + 1);
         a->ticket = ticket;
     }
     return FS_OK;
@@ -825,7 +849,7 @@ fs_status plan_scan(int64_t n, int32_t D, fs_dtype dtype, int32_t T, int32_t B, 
 fs_status clear_words(const ScanArgs& a, int N, int values, hipStream_t s)
 {
     if (a.tiles <= 1) return FS_OK;
-    const int64_t pieces = (a.tiles + a.tiles / kSpan) * a.col_blocks * (a.lanes * N / 2);      // at least 2 a tile
+    const int64_t pieces = (a.tiles + a.tiles / kSpan) * a.col_blocks * (a.lanes * N / 2);      // at least 2 a tile, of 2 tiles or more
     const int64_t grid = (pieces + kBlock - 1) / kBlock;                    // fewer than the tiles' workgroups, in plan_scan's bound
     FS_LAUNCH("scan_clear", scan_clear_kernel, dim3((unsigned)grid), dim3(kBlock), s, a, pieces, a.groups * (values / N));
     return FS_OK;
