@@ -467,24 +467,20 @@ constexpr int kSmallRounds = 8;              // rounds of one workgroup over all
 // lane fewer lanes lie past the row's end, and rows of more instructions apart in time share more cache lines.  Bf16, 0.8 GB, us:
 // forward rows of 40 pieces (64, 1) 313, (16, 3) 265; 150 (64, 4) 473, (64, 3) 292; 600 (256, 4) 342, (256, 3) 287; but 17
 // (32, 1) 342, (8, 3) 476.
-#define FS_DISPATCH_ROW(units, CALL)                                                    \
+#define FS_DISPATCH_FWD_ROW(units, CALL)                                                \
     do {                                                                                \
-        if ((units) > 512) { CALL(256, 4); }                                            \
+        if ((units) > 768) { CALL(256, 4); }                                            \
+        else if ((units) > 512) { CALL(256, 3); }                                       \
         else if ((units) > 256) { CALL(256, 2); }                                       \
-        else if ((units) > 128) { CALL(64, 4); }                                        \
+        else if ((units) > 192) { CALL(64, 4); }                                        \
+        else if ((units) > 128) { CALL(64, 3); }                                        \
         else if ((units) > 64) { CALL(64, 2); }                                         \
-        else if ((units) > 32) { CALL(64, 1); }                                         \
+        else if ((units) > 48) { CALL(64, 1); }                                         \
+        else if ((units) > 32) { CALL(16, 3); }                                         \
         else if ((units) > 16) { CALL(32, 1); }                                         \
         else if ((units) > 8) { CALL(16, 1); }                                          \
         else if ((units) > 4) { CALL(8, 1); }                                           \
         else { CALL(4, 1); }                                                            \
-    } while (0)
-#define FS_DISPATCH_FWD_ROW(units, CALL)                                                \
-    do {                                                                                \
-        if ((units) > 512 && (units) <= 768) { CALL(256, 3); }                          \
-        else if ((units) > 128 && (units) <= 192) { CALL(64, 3); }                      \
-        else if ((units) > 32 && (units) <= 48) { CALL(16, 3); }                        \
-        else FS_DISPATCH_ROW(units, CALL);                                              \
     } while (0)
 // Backward fewer lanes a row still: what a lane does beside its columns (the sums over the lanes, the row's statistics and
 // places) is shared by more of them.  From the checkpoint, bf16, 0.4 G values, us: 40 pieces (64, 1) 562, (16, 3) 346; 64 (64, 1) 377,
@@ -494,15 +490,26 @@ constexpr int kSmallRounds = 8;              // rounds of one workgroup over all
 // its checkpoint (32, 1) 432, (8, 3) 479.
 #define FS_DISPATCH_BWD_ROW(units, few, CALL)                                           \
     do {                                                                                \
-        if ((units) > 512 && (units) <= 768) { CALL(256, 3); }                          \
-        else if ((units) > 96 && (units) <= 128) { CALL(32, 4); }                       \
-        else if ((units) > 64 && (units) <= 96) { CALL(32, 3); }                        \
-        else if ((units) > 48 && (units) <= 64) { CALL(32, 2); }                        \
-        else if ((units) > 32 && (units) <= 48) { CALL(16, 3); }                        \
-        else if ((few) && (units) > 24 && (units) <= 32) { CALL(16, 2); }               \
-        else if ((few) && (units) > 16 && (units) <= 24) { CALL(8, 3); }                \
-        else if ((few) && (units) > 8 && (units) <= 16) { CALL(8, 2); }                 \
-        else FS_DISPATCH_ROW(units, CALL);                                              \
+        if ((units) > 768) { CALL(256, 4); }                                            \
+        else if ((units) > 512) { CALL(256, 3); }                                       \
+        else if ((units) > 256) { CALL(256, 2); }                                       \
+        else if ((units) > 128) { CALL(64, 4); }                                        \
+        else if ((units) > 96) { CALL(32, 4); }                                         \
+        else if ((units) > 64) { CALL(32, 3); }                                         \
+        else if ((units) > 48) { CALL(32, 2); }                                         \
+        else if ((units) > 32) { CALL(16, 3); }                                         \
+        else if constexpr (few) {                                                       \
+            if ((units) > 24) { CALL(16, 2); }                                          \
+            else if ((units) > 16) { CALL(8, 3); }                                      \
+            else if ((units) > 8) { CALL(8, 2); }                                       \
+            else if ((units) > 4) { CALL(8, 1); }                                       \
+            else { CALL(4, 1); }                                                        \
+        } else {                                                                        \
+            if ((units) > 16) { CALL(32, 1); }                                          \
+            else if ((units) > 8) { CALL(16, 1); }                                      \
+            else if ((units) > 4) { CALL(8, 1); }                                       \
+            else { CALL(4, 1); }                                                        \
+        }                                                                               \
     } while (0)
 
 // Rows that a group has in flight.  Forward 2 (3.93 M rows of 256 bf16: 1, 2, 4, 8 rows 728, 691, 718, 718 us; rows of 1024 pieces 1, 2
@@ -512,12 +519,15 @@ constexpr int kFwdRows = 2;
 constexpr int bwd_rows(int G, int P) { return P == 1 ? 4 : G > kWave && P == 2 ? 2 : 1; }
 
 // Rows of a workgroup's round in the backward pass.
-int64_t bwd_round(int units, bool few)
+template <bool FEW>
+int64_t bwd_round_of(int units)
 {
 #define CALL(G, P) return (int64_t)(kBlock / G) * bwd_rows(G, P)
-    FS_DISPATCH_BWD_ROW(units, few, CALL);
+    FS_DISPATCH_BWD_ROW(units, FEW, CALL);
 #undef CALL
 }
+
+int64_t bwd_round(int units, bool few) { return few ? bwd_round_of<true>(units) : bwd_round_of<false>(units); }
 
 int64_t bwd_blocks(int64_t n, int units, bool few)
 {
