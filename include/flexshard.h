@@ -596,13 +596,17 @@ fs_status fs_seq_unpack8(
  *   gamma[D], beta[D], mean[n], rstd[n] are float32.  mean and rstd (both or
  *   neither) are what the backward pass needs; codes and exps (both or neither)
  *   receive x as fs_seq_pack8 writes it, in the same pass.  y may be x.
+ *   A row with an infinity or a NaN has NaN in rstd and y, and in mean what its
+ *   sum says (an infinity, or NaN); no other row is touched by it.  Sums of x and
+ *   of squared deviations past float32 count as infinite.
  * fs_seq_norm_bwd -- with u = (x - mean) rstd and g = dy gamma:
  *   dx[i, d] = rstd[i] (g[i, d] - sum_d g / D - u[i, d] sum_d g u / D),
  *   dgamma[d] = sum_i dy[i, d] u[i, d],  dbeta[d] = sum_i dy[i, d]   (overwritten)
  *   dx may be dy.  The same bits on every run (no atomics).
  * fs_seq_norm_bwd_packed -- the same with x given as a checkpoint (codes, exps
- *   of fs_seq_pack8 or fs_seq_norm_fwd); mean and rstd are those of the rows
- *   themselves.  Both ask for the same workspace.
+ *   of fs_seq_pack8 or fs_seq_norm_fwd), its values as they are in fp32 (not held
+ *   to fp16's range); mean and rstd are those of the rows themselves.  Both ask
+ *   for the same workspace.
  *   Host faults: unknown dtype; n < 0, n >= 2^31, D < 1, a row of 4 MB or more
  *   (FS_ERR_SIZE); eps not positive and finite (FS_ERR_CONFIG); NULL; alignment
  *   as above, gamma and beta 16-byte aligned too; workspace as everywhere.
@@ -633,8 +637,10 @@ fs_status fs_seq_norm_bwd_packed(
  *   h[n, D] in `dtype`; the recurrence itself runs on unrounded float32 states.
  *   h0[T*B, D], h_last[T*B, D] float32; h_last (may be NULL) = the state after
  *   the last row, of an empty sequence its h0 (or 0).  A gate of -infinity
- *   shuts out the state before it, one of +infinity keeps it.  h may be x,
- *   h_last may be h0.
+ *   shuts out the (finite) state before it, one of +infinity keeps it.  f_t and
+ *   1 - f_t are within |gate| + 16 roundings of float32 (below its normal numbers
+ *   they may be 0).  A state that is infinite or NaN leaves the rest of its
+ *   sequence so, one or the other.  h may be x, h_last may be h0.
  * fs_seq_scan_bwd -- gradients for dh[n, D] (of h) and dh_last (of h_last, may
  *   be NULL = 0), backwards along every sequence:
  *   G_t = dh_t + f_(t+1) G_(t+1)  (the last row: dh_t + dh_last[s]),
@@ -644,8 +650,9 @@ fs_status fs_seq_norm_bwd_packed(
  *   `dtype`, h0 of the first row in float32).  dx or dgate may be dh, dh0 may
  *   be dh_last.
  * fs_seq_scan_bwd_packed -- the same with x, gate and h given as checkpoints of
- *   fs_seq_pack8: 3 bytes a value and column held for the backward pass
- *   instead of 6 or 12.
+ *   fs_seq_pack8, their values as they are in fp32: 3 bytes a row and column held
+ *   for the backward pass instead of 6 or 12.  Making them is three passes more
+ *   over the rows.
  * fs_seq_scan_step -- one row for each of m sequences (serving a token at a
  *   time): state_out = f state + (1 - f) x, h = state_out in `dtype`.
  *   state[m, D], state_out[m, D] float32; state_out may be state, h may be x.
@@ -657,13 +664,14 @@ fs_status fs_seq_norm_bwd_packed(
  * The same bits on every run, from one workspace or another: the recurrence
  * is put together from stretches of rows that n and D alone decide.
  * Workspace (not for the step): 8 bytes a column for every stretch of rows
- * that a workgroup has at a time, less than 4 % of x forward and 8 % backward;
- * nothing in it has to survive from call to call or start at any value.
+ * that a workgroup has at a time, less than 7.5 % of x forward and 15 % backward
+ * (float32: half of that), 8 bytes a column and 1 KB more; nothing in it has to
+ * survive from call to call or start at any value.
  * Host faults: unknown dtype; n < 0, n >= 2^31, D < 1, T < 1, B < 1,
  * T*B >= 2^31, a row of 4 MB or more, more than 2^24 - 1 stretches of rows and
- * columns (over 240 GB in x), for the step over 64 GB in x (FS_ERR_SIZE); NULL;
- * alignment as above, h0, h_last, dh_last, dh0 and the states 16-byte aligned
- * too; workspace as everywhere.
+ * columns (over 240 GB in x), for the step instead of these two over 64 GB in x
+ * (FS_ERR_SIZE); NULL; alignment as above, h0, h_last, dh_last, dh0 and the
+ * states 16-byte aligned too; workspace as everywhere.
  */
 fs_status fs_seq_scan_fwd(
     const void* x, const void* gate, int64_t n, int32_t D, fs_dtype dtype,

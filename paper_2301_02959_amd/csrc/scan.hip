@@ -17,11 +17,12 @@
 // atomics at the scope of the GPU, nothing else is passed on), cleared by a launch in front.
 //
 // Measured (us, and the rate of what has to be read and written; a large copy runs at 6.2 TB/s, torch's own at 5.1): 4.2 M rows of 128
-// in 32768 sequences, forward fp16 544 (5.9 TB/s), backward bf16 1098 (5.9); 83 k rows of 128 bf16 in 692 sequences 26 (2.5),
-// which is the time of one tile from its number to its last store; three sequences of 100 k rows of 64 fp32 63 (3.7): 1172 tiles
-// for 768 places; 523 k rows of 256 fp16 backward from checkpoints 310 (4.3).  The traffic is the least possible within 4 %
-// forward (the words) and 4 % backward (the words, h of the row before every tile).  One workgroup a sequence instead took
-// 1041, 1547, 559, 47950 and 5198.
+// in 32768 sequences, forward fp16 544 (5.9 TB/s), backward bf16 1098 (5.9); 80.5 k rows of 128 bf16 in 692 sequences 26 (2.4),
+// which is the time of one tile from its number to its last store; 284 k rows of 64 fp32 in three sequences 63 (3.5): 1111 tiles
+// for 768 places; 556 k rows of 256 fp16 backward from checkpoints 310 (4.2).  The traffic of the first two is the least possible
+// within 4 % (the words; backward h of the row before every tile too); rows of 19 pieces and more that are no multiple of 8 have
+// shorter tiles, whose words are up to 7.3 % of x forward and 14.5 % backward.  One workgroup a sequence instead took 1041, 1547, 559,
+// 47950 and 5198.
 #include <type_traits>
 
 #include "pack8.h"
@@ -59,7 +60,8 @@ struct ScanArgs {
     uint32_t* ticket;                // null: one tile, nothing to wait for
 };
 
-// f and 1 - f of a gate, each to the precision of e^-gate (1 - f is not taken from f, which is 1 for large gates).
+// f and 1 - f of a gate, each to the precision of e^-gate (1 - f is not taken from f, which is 1 for large gates).  That is the
+// exponential's own and up to |gate| roundings: its argument is a rounded product, and an exponent off by d takes e^d.
 __device__ __forceinline__ void gate_pair(float gate, float* f, float* o)
 {
     const float e = __builtin_amdgcn_exp2f(gate * -1.44269504f);

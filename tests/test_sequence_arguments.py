@@ -165,3 +165,17 @@ def test_a_workspace_without_bytes_is_too_small():
         assert call(raise_on_error=False) == 5
         with pytest.raises(fs.FlexShardError):
             call()
+
+
+@pytest.mark.parametrize("dtype, N, forward, backward", [(0, 4, 0.0375, 0.075), (1, 8, 0.075, 0.15), (2, 8, 0.075, 0.15)])
+def test_the_recurrences_workspace_stays_under_what_the_header_says(dtype, N, forward, backward):
+    """... of x, and 8 bytes a column and 1 KB: a caller may size a pool by it."""
+    for units in list(range(1, 300)) + [449, 450, 1000, 1025, 4095, 4097, 65537, 99999, (1 << 18) - 1]:
+        D = units * N
+        for n in (0, 1, 31, 33, 65, 129, 257, 513, 1025, 4100, 100_000, 4_000_000):
+            x = 16 * n * units
+            if x > 200 * 10 ** 9:
+                continue
+            for size, share in ((fs.seq_scan_fwd_workspace_bytes, forward), (fs.seq_scan_bwd_workspace_bytes, backward)):
+                for S in (1, 70_000):
+                    assert size(n, D, dtype, 1, S) <= share * x + 8 * D + 1024, (n, D)
