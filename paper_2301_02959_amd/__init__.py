@@ -532,7 +532,7 @@ def _rows(fn: str, kinds: str, rows: torch.Tensor, *tensors, sequences: int = 0)
     on its device, which has to be the current one (the stream is).  The library takes sizes from the caller, so a tensor that is
     too small would be read past its end.  A letter of `kinds` for each tensor, which may be None: s [n, D] of the type of rows;
     f [n, D], c [D], r [n], t [sequences, D] float32; p [n, D] codes and e [n, ceil(D / 32)] exponents of a checkpoint;
-    o [sequences + 1] offsets."""
+    o [sequences + 1] offsets; w a workspace and i a status word, on that device too."""
     if _fit is not None and rows.is_cuda:
         got = _fit(kinds, _raw_device(), sequences, rows, *tensors)
         if got is not None:
@@ -553,6 +553,11 @@ def _rows_checked(fn: str, kinds: str, rows: torch.Tensor, tensors: tuple, seque
               "p": ((n, D), torch.int8), "e": ((n, (D + 31) // 32), torch.uint8), "o": ((sequences + 1,), torch.int64),
               "t": ((sequences, D), torch.float32)}
     for kind, t in zip(kinds, tensors):
+        if kind in "wi":
+            _ptr(t, _I32 if kind == "i" else None)
+            if t is not None and t.get_device() != where:
+                raise ValueError(f"{fn}: got a tensor on {t.device}, the rows are on {rows.device}")
+            continue
         shape, dtype = wanted[kind]
         if t is not None and (tuple(t.shape) != shape or t.dtype != dtype or t.get_device() != where):
             raise ValueError(f"{fn}: expected {dtype} of shape {shape} on the device of the rows, got {t.dtype} {tuple(t.shape)} on {t.device}")
@@ -587,41 +592,34 @@ def fs_seq_norm_fwd(x, gamma, beta, eps: float, y, mean=None, rstd=None, codes=N
     return _check("fs_seq_norm_fwd", code, raise_on_error)
 
 
-def _ptr_here(fn: str, t: Optional[torch.Tensor], dtypes: Optional[tuple] = None) -> Optional[int]:
-    """_ptr of a workspace or a status word, which has to be on the current device as _rows finds the operands to be."""
-    pointer = _ptr(t, dtypes)
-    if t is not None and t.get_device() != _raw_device():
-        raise ValueError(f"{fn}: got a tensor on {t.device}, the current device is {_raw_device()}")
-    return pointer
-
-
-def _with_workspace(fn: str, entry, args: tuple, tail: tuple, device, workspace: Optional[torch.Tensor], raise_on_error: bool) -> int:
+def _with_workspace(fn: str, entry, args: tuple, tail: tuple, device, workspace: Optional[torch.Tensor], pointer: Optional[int],
+                    raise_on_error: bool) -> int:
     """entry(*args, workspace, its size, *tail) with the caller's workspace, or one of the size that the entry point asks for."""
     if workspace is None:
         workspace, size, code = _workspace(lambda ws, size: entry(*args, ws, size, *tail), device)
         if code != 0:
             return _check(fn, code, raise_on_error)
+        pointer = _ptr(workspace)
     else:
         size = ctypes.c_size_t(workspace.numel() * workspace.element_size())
-    pointer = _ptr_here(fn, workspace)
-    if not pointer:                              # a workspace of no bytes: the library would take it for the question
-        return _check(fn, FS_ERR_WORKSPACE, raise_on_error)
+        if not pointer:                          # a workspace of no bytes: the library would take it for the question
+            return _check(fn, FS_ERR_WORKSPACE, raise_on_error)
     return _check(fn, entry(*args, pointer, ctypes.byref(size), *tail), raise_on_error)
 
 
 def fs_seq_norm_bwd(dy, x, mean, rstd, gamma, dx, dgamma, dbeta, workspace: Optional[torch.Tensor] = None,
                     raise_on_error: bool = True) -> int:
-    n, D, dtype, dy_, x_, mean_, rstd_, *rest = _rows("fs_seq_norm_bwd", "srrcscc", dy, x, mean, rstd, gamma, dx, dgamma, dbeta)
+    n, D, dtype, dy_, x_, mean_, rstd_, *rest, ws_ = _rows("fs_seq_norm_bwd", "srrcsccw", dy, x, mean, rstd, gamma, dx, dgamma, dbeta, workspace)
     return _with_workspace("fs_seq_norm_bwd", _typed().fs_seq_norm_bwd, (dy_, x_, mean_, rstd_, n, D, dtype, *rest), (_stream(),),
-                           dy.device, workspace, raise_on_error)
+                           dy.device, workspace, ws_, raise_on_error)
 
 
 def fs_seq_norm_bwd_packed(dy, codes, exps, mean, rstd, gamma, dx, dgamma, dbeta, workspace: Optional[torch.Tensor] = None,
                            raise_on_error: bool = True) -> int:
-    n, D, dtype, dy_, codes_, exps_, mean_, rstd_, *rest = _rows("fs_seq_norm_bwd_packed", "perrcscc", dy, codes, exps, mean, rstd, gamma,
-                                                                 dx, dgamma, dbeta)
+    n, D, dtype, dy_, codes_, exps_, mean_, rstd_, *rest, ws_ = _rows("fs_seq_norm_bwd_packed", "perrcsccw", dy, codes, exps, mean, rstd, gamma,
+                                                                      dx, dgamma, dbeta, workspace)
     return _with_workspace("fs_seq_norm_bwd_packed", _typed().fs_seq_norm_bwd_packed,
-                           (dy_, codes_, exps_, mean_, rstd_, n, D, dtype, *rest), (_stream(),), dy.device, workspace, raise_on_error)
+                           (dy_, codes_, exps_, mean_, rstd_, n, D, dtype, *rest), (_stream(),), dy.device, workspace, ws_, raise_on_error)
 
 
 def seq_norm_bwd_workspace_bytes(n: int, D: int, dtype: int) -> int:
@@ -635,28 +633,29 @@ def seq_norm_bwd_workspace_bytes(n: int, D: int, dtype: int) -> int:
 def fs_seq_scan_fwd(x, gate, offsets, T: int, B: int, h0, h, h_last=None, dev_status=None,
                     workspace: Optional[torch.Tensor] = None, raise_on_error: bool = True) -> int:
     T, B, S = _tables(T, B)
-    n, D, dtype, x_, gate_, offsets_, h0_, h_, last_ = _rows("fs_seq_scan_fwd", "sotst", x, gate, offsets, h0, h, h_last, sequences=S)
+    n, D, dtype, x_, gate_, offsets_, h0_, h_, last_, ws_, status_ = _rows("fs_seq_scan_fwd", "sotstwi", x, gate, offsets, h0, h, h_last,
+                                                                           workspace, dev_status, sequences=S)
     return _with_workspace("fs_seq_scan_fwd", _typed().fs_seq_scan_fwd, (x_, gate_, n, D, dtype, offsets_, T, B, h0_, h_, last_),
-                           (_stream(), _ptr_here("fs_seq_scan_fwd", dev_status, _I32)), x.device, workspace, raise_on_error)
+                           (_stream(), status_), x.device, workspace, ws_, raise_on_error)
 
 
 def fs_seq_scan_bwd(dh, dh_last, x, gate, h, offsets, T: int, B: int, h0, dx, dgate, dh0=None, dev_status=None,
                     workspace: Optional[torch.Tensor] = None, raise_on_error: bool = True) -> int:
     T, B, S = _tables(T, B)
-    n, D, dtype, dh_, last_, x_, gate_, h_, offsets_, *rest = _rows("fs_seq_scan_bwd", "tsssotsst", dh, dh_last, x, gate, h, offsets, h0, dx, dgate,
-                                                                    dh0, sequences=S)
+    n, D, dtype, dh_, last_, x_, gate_, h_, offsets_, *rest, ws_, status_ = _rows("fs_seq_scan_bwd", "tsssotsstwi", dh, dh_last, x, gate, h, offsets,
+                                                                                  h0, dx, dgate, dh0, workspace, dev_status, sequences=S)
     return _with_workspace("fs_seq_scan_bwd", _typed().fs_seq_scan_bwd, (dh_, last_, x_, gate_, h_, n, D, dtype, offsets_, T, B, *rest),
-                           (_stream(), _ptr_here("fs_seq_scan_bwd", dev_status, _I32)), dh.device, workspace, raise_on_error)
+                           (_stream(), status_), dh.device, workspace, ws_, raise_on_error)
 
 
 def fs_seq_scan_bwd_packed(dh, dh_last, x_codes, x_exps, gate_codes, gate_exps, h_codes, h_exps, offsets, T: int, B: int,
                            h0, dx, dgate, dh0=None, dev_status=None, workspace: Optional[torch.Tensor] = None,
                            raise_on_error: bool = True) -> int:
     T, B, S = _tables(T, B)
-    n, D, dtype, *got = _rows("fs_seq_scan_bwd_packed", "tpepepeotsst", dh, dh_last, x_codes, x_exps, gate_codes, gate_exps, h_codes, h_exps,
-                              offsets, h0, dx, dgate, dh0, sequences=S)
+    n, D, dtype, *got, ws_, status_ = _rows("fs_seq_scan_bwd_packed", "tpepepeotsstwi", dh, dh_last, x_codes, x_exps, gate_codes, gate_exps, h_codes,
+                                            h_exps, offsets, h0, dx, dgate, dh0, workspace, dev_status, sequences=S)
     return _with_workspace("fs_seq_scan_bwd_packed", _typed().fs_seq_scan_bwd_packed, (*got[:8], n, D, dtype, got[8], T, B, *got[9:]),
-                           (_stream(), _ptr_here("fs_seq_scan_bwd_packed", dev_status, _I32)), dh.device, workspace, raise_on_error)
+                           (_stream(), status_), dh.device, workspace, ws_, raise_on_error)
 
 
 def seq_scan_fwd_workspace_bytes(n: int, D: int, dtype: int, T: int, B: int) -> int:

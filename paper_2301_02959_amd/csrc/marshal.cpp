@@ -62,10 +62,20 @@ static bool fits(PyObject* obj, int64_t device, at::ScalarType type, int dims, i
     return *pointer != nullptr;
 }
 
+// Whether `obj` is a plain contiguous tensor on CUDA device `device`, of whatever sizes; of int32 where `words` is set.
+static bool is_here(PyObject* obj, int64_t device, bool words, PyObject** pointer)
+{
+    if (!THPVariable_CheckExact(obj)) return false;
+    const at::Tensor& t = THPVariable_Unpack(obj);
+    if (!t.is_cuda() || t.get_device() != device || !t.is_contiguous() || (words && t.scalar_type() != at::kInt)) return false;
+    *pointer = PyLong_FromUnsignedLongLong(reinterpret_cast<unsigned long long>(t.data_ptr()));
+    return *pointer != nullptr;
+}
+
 // rows_that_fit(kinds, device, sequences, rows, *tensors) -> (n, D, type, pointer of rows, pointers ...), or None where Python has
 // to look.  rows: [n, D]; kinds: a letter for each tensor, which may be None:
 //   s [n, D] as rows   f [n, D] float32   c [D] float32   r [n] float32   p [n, D] int8   e [n, ceil(D / 32)] uint8
-//   o [sequences + 1] int64   t [sequences, D] float32
+//   o [sequences + 1] int64   t [sequences, D] float32   w a workspace, of any type and sizes   i int32 words of any sizes
 static PyObject* rows_that_fit(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 {
     if (nargs < 4 || !PyUnicode_Check(args[0]) || !PyLong_Check(args[1]) || !PyLong_Check(args[2])) Py_RETURN_NONE;
@@ -106,6 +116,8 @@ static PyObject* rows_that_fit(PyObject*, PyObject* const* args, Py_ssize_t narg
                     case 'e': ok = fits(obj, device, at::kByte, 2, n, (D + 31) / 32, &pointer); break;
                     case 'o': ok = fits(obj, device, at::kLong, 1, S + 1, 0, &pointer); break;
                     case 't': ok = fits(obj, device, at::kFloat, 2, S, D, &pointer); break;
+                    case 'w': ok = is_here(obj, device, false, &pointer); break;
+                    case 'i': ok = is_here(obj, device, true, &pointer); break;
                     default: ok = false;
                 }
             }

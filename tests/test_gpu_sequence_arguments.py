@@ -44,3 +44,24 @@ def test_wide_rows_in_many_sequences(S):
         got.append((h, dx, dg))
     for a, b in zip(*got):
         assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+def test_workspaces_and_status_words_in_native_code_and_in_python():
+    """Any type and sizes of a workspace, int32 words; both on the rows' device, contiguous.  What the native look does not take
+    the one in Python refuses."""
+    x = torch.zeros(6, 64, device=DEV)
+    for ws in (torch.empty(300, dtype=torch.uint8, device=DEV), torch.empty(3, 5, device=DEV), torch.empty(0, device=DEV), None):
+        for st in (torch.zeros(1, dtype=torch.int32, device=DEV), torch.zeros(2, 3, dtype=torch.int32, device=DEV), None):
+            assert fs._fit("wi", 0, 0, x, ws, st) == fs._rows_checked("test", "wi", x, (ws, st), 0)
+    good, word = torch.empty(300, dtype=torch.uint8, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    for ws, st in ((good.cpu(), word), (torch.empty(9, 9, device=DEV).t(), word), (good[::2], word), (good, word.cpu()), (good, word.long()),
+                   (good, torch.zeros(4, dtype=torch.int32, device=DEV)[::2]), ("text", word)):
+        assert fs._fit("wi", 0, 0, x, ws, st) is None
+        with pytest.raises((TypeError, AttributeError)):
+            fs._rows_checked("test", "wi", x, (ws, st), 0)
+    assert fs._fit("w", 1, 0, x, good) is None
+
+    class Sub(torch.Tensor):
+        pass
+
+    assert fs._rows("test", "w", x, good.as_subclass(Sub)) == fs._rows("test", "w", x, good)
