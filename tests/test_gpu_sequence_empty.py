@@ -62,3 +62,29 @@ def test_bad_offsets_of_many_sequences_stay_in_bounds(D):
             assert int(st.item()) == fs.FS_DEV_BAD_OFFSETS
             for t in (h, dx, dg, last, d0):
                 assert (t[0] == 3).all() and (t[-1] == 3).all()
+
+
+@pytest.mark.parametrize("dtype, D", [(torch.bfloat16, 8), (torch.float32, 64), (torch.float16, 136)])
+def test_the_most_sequences_a_call_admits(dtype, D):
+    """2^31 - 1 sequences, four of them with rows: the bits of a batch of those four."""
+    S, at = (1 << 31) - 1, {0: 200, 7: 3, 1 << 30: 500, (1 << 31) - 2: 64}
+    few = torch.from_numpy(offsets_of(list(at.values()))).to(DEV)
+    n = int(few[-1])
+    many = torch.empty(S + 1, dtype=torch.int64, device=DEV)
+    edges = [0] + [s + 1 for s in at] + [S + 1]
+    for i in range(len(edges) - 1):
+        many[edges[i]:edges[i + 1]] = int(few[i])
+    assert int(many[-1]) == n
+    x, gate, dh = (torch.randn(n, D, device=DEV).to(dtype) for _ in range(3))
+    got = []
+    for off, T, B in ((few, 4, 1), (many, 1, S)):
+        st = torch.zeros(1, dtype=torch.int32, device=DEV)
+        h, dx, dg = (torch.full_like(x, 7.0) for _ in range(3))
+        fs.fs_seq_scan_fwd(x, gate, off, T, B, None, h, None, st)
+        fs.fs_seq_scan_bwd(dh, None, x, gate, h, off, T, B, None, dx, dg, None, st)
+        assert int(st.item()) == 0
+        got.append((h, dx, dg))
+    for a, b in zip(*got):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    del many
+    torch.cuda.empty_cache()
